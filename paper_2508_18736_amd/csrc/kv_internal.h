@@ -1,0 +1,114 @@
+// What the translation units of the paged key/value cache share (siso_kv.h).
+#pragma once
+
+#include "siso_internal.h"
+#include "siso_kv.h"
+
+// How a page lies in memory.  Attention multiplies 32 x 32 tiles with v_mfma_f32_32x32x16_bf16: S^T = K Q^T, then O^T = V^T P^T.
+// Keys and values are kept in the order in which the lanes of these products want them, in blocks of 16 tokens, so that
+// a wave loads an operand as whole lines, 16 bytes a lane, straight to registers or LDS, and no product transposes anything.
+//   K: 16-byte chunks [chunk of the dimension][token]: lane l of a fragment takes token l % 16 of one of two blocks and every
+//      second chunk from l / 32 on.  A chunk is 8 elements of 16 bits or 16 codes: one fragment or two.
+//   V: the accumulator of S^T holds, in lane half h, tokens 4 h + j and 8 + 4 h + j (j < 4) of a block: as they are, these
+//      eight are an operand of the second product.  V is kept as [h][dimension][these eight tokens] (16 bits: 16 bytes); codes as
+//      [h][dimension / 64][32][two 32s of the dimension][eight tokens], again 16 bytes for a lane: two fragments.
+// The dimension is rounded up to a multiple of 64; what lies beyond it is zero from siso_kv_create on and never written.
+#define SISO_KV_BLOCK 16
+__host__ __device__ __forceinline__ int kv_slot(int key) { return (key & 3) + 4 * (key >> 3); }  // of a block's token among the eight of its half
+__host__ __device__ __forceinline__ int kv_half(int key) { return (key >> 2) & 1; }
+
+// Pools: [layer][page][kv head][page_tokens * dp * (2 or 1) bytes], blocks one after the other; scales [layer][page][kv head][page_tokens].
+struct KvPool {
+    char *k, *v;
+    float *ks, *vs;  // NULL: 16 bits
+    u64 *bad;
+    long pages;
+    int kv_heads, shift;  // page_tokens = 1 << shift
+    int dim, dp;
+};
+
+struct KvBatch {  // siso_kv_batch as kernels take it
+    const int *first, *length, *pages;
+    int n, rows;
+    long width;
+    int most;  // the longest length there can be: width * page_tokens
+    int single;  // every sequence has exactly one row
+};
+
+// Sequences' rows in groups of 1 << shift, `group` of a row's units each (attention: query heads that share a kv head): group
+// number j of sequence b is slot kv_slots_before(b) + j, for every sequence as many slots as it may have groups and `extra`
+// more.  Nothing but the rows before a sequence decides where its slots begin: no launch before that one counts them.
+__host__ __device__ __forceinline__ long kv_slots_before(long first, long b, int group, int shift, int extra) {
+    return ((first * group) >> shift) + b * extra;
+}
+
+#ifdef __HIPCC__
+struct KvSequence {
+    int b, first, rows, length;
+    int start;  // position of the first row; may be below zero
+};
+
+__device__ __forceinline__ int kv_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+__device__ __forceinline__ KvSequence kv_sequence(const KvBatch &batch, int b) {
+    KvSequence s;
+    s.b = b;
+    s.first = kv_clamp(batch.first[b], 0, batch.rows);
+    s.rows = kv_clamp(batch.first[b + 1], s.first, batch.rows) - s.first;
+    s.length = batch.length ? kv_clamp(batch.length[b], 0, batch.most) : 0;
+    s.start = s.length - s.rows;
+    return s;
+}
+
+// The sequence that `slot` belongs to, the same in every lane: the wave looks at 64 sequences at a time.
+__device__ __forceinline__ int kv_sequence_of(const KvBatch &batch, long slot, int group, int shift, int extra) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, count = batch.n;
+    while (count > 1) {
+        const int step = (count + 63) / 64, at = lo + lane * step;
+        const bool before = lane * step < count && kv_slots_before(kv_clamp(batch.first[at], 0, batch.rows), at, group, shift, extra) <= slot;
+        const int k = __popcll(__ballot(before));  // (not decreasing: those before come first)
+        lo += (k > 0 ? k - 1 : 0) * step;
+        count = batch.n - lo < step ? batch.n - lo : step;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// The page of position `at` (below most, the same in every lane), or -1.
+__device__ __forceinline__ long kv_page(const KvPool &pool, const KvBatch &batch, int b, int at) {
+    const int page = __builtin_amdgcn_readfirstlane(batch.pages[(long)b * batch.width + (at >> pool.shift)]);
+    return (unsigned)page < (unsigned long)pool.pages ? page : -1;
+}
+// Where the block of position `at` of a kv head begins, in bytes for elements of one byte (16 bits: twice that).
+__device__ __forceinline__ size_t kv_block_at(const KvPool &pool, long page, int head, int at) {
+    return ((size_t)(page * pool.kv_heads + head) << pool.shift) * pool.dp + (size_t)(((at & ((1 << pool.shift) - 1)) >> 4) * SISO_KV_BLOCK) * pool.dp;
+}
+__device__ __forceinline__ size_t kv_scale_at(const KvPool &pool, long page, int head, int at) {
+    return ((size_t)(page * pool.kv_heads + head) << pool.shift) + (at & ((1 << pool.shift) - 1));
+}
+#endif
+
+struct siso_kv {
+    int layers, kv_heads, dim, dp, page_tokens, dtype;
+    long pages;
+    hipStream_t stream;
+    char *k, *v;
+    float *ks, *vs;
+    size_t layer_bytes, layer_scales;
+    u64 *counters;  // [0] page numbers that are none
+    u64 *host_pin;
+    float *parts;  // what splits of a long axis leave for the one that joins them; see kv_attend.hip and kv_verify.hip
+    size_t parts_floats;
+    char err[256];
+};
+
+int kv_fail(siso_kv *kv, int code, const char *fmt, ...);
+int kv_check_hip(siso_kv *kv, hipError_t e, const char *what);
+#define KV_TRY(kv, call)                                           \
+    do {                                                           \
+        const int kv_rc_ = kv_check_hip((kv), (call), #call);      \
+        if (kv_rc_ != SISO_OK) return kv_rc_;                      \
+    } while (0)
+KvPool kv_pool(const siso_kv *kv, int layer);
+// Checks a batch for a call that reads the cache (or, layer < 0, does not) and brings it into the kernels' form.
+int kv_batch(siso_kv *kv, const char *call, int layer, const siso_kv_batch *batch, KvBatch *out);

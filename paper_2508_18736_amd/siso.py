@@ -1,5 +1,5 @@
-"""Thin binding over the C-ABI library ``libsiso.so`` (declared in ``include/siso.h``; the tuning and
-timing calls in ``include/siso_bench.h``).
+"""Thin binding over the C-ABI library ``libsiso.so`` (declared in ``include/siso.h``; the paged key/value
+cache in ``include/siso_kv.h``; the tuning and timing calls in ``include/siso_bench.h``).
 
 Argument marshalling only: every step of the hot path runs in the library's HIP
 kernels.  PyTorch supplies device memory (``tensor.data_ptr()``) and the stream.
@@ -71,6 +71,15 @@ SYMBOLS = {
     "siso_md1_wait": ([C.c_double, C.c_double, C.c_double], C.c_double),
     "siso_pick_threshold": ([_vp, _vp, _it, C.c_double, C.c_double, C.c_double, C.POINTER(_it)], _it),
     "siso_adjust_threshold": ([_vp, _it, _it, C.c_double, C.c_double], _it),
+    "siso_kv_create": ([_it, _it, _it, _it, _lg, _it, C.POINTER(_vp)], _it),
+    "siso_kv_destroy": ([_vp], None),
+    "siso_kv_set_stream": ([_vp, _vp], _it),
+    "siso_kv_write": ([_vp, _it, _vp, _vp, _lg, _lg, _vp, _lg, _lg], _it),
+    "siso_kv_read": ([_vp, _it, _vp, _it, _vp, _vp], _it),
+    "siso_kv_attend": ([_vp, _it, _vp, _vp, _lg, _lg, _it, _fl, _it, _vp, _vp], _it),
+    "siso_kv_verify": ([_vp, _vp, _vp, _it, _it, _vp, _lg, _vp, _lg, _vp, _vp, _vp, _vp], _it),
+    "siso_kv_bad_pages": ([_vp], _lg),
+    "siso_kv_last_error": ([_vp], C.c_char_p),
 }
 for _name, (_args, _res) in SYMBOLS.items():
     _fn = getattr(_lib, _name)
@@ -477,3 +486,163 @@ class SisoCache:
         sizes = torch.empty(k, dtype=torch.int32, device=self.device)
         self._check(_lib.siso_export(self._h, _ptr(cents), _ptr(means), _ptr(sizes)))
         return cents, means, sizes
+
+
+class _KvBatchStruct(C.Structure):
+    _fields_ = [("n", _lg), ("rows", _lg), ("first", _vp), ("length", _vp), ("pages", _vp), ("width", _lg), ("max_new", _lg),
+                ("max_length", _lg)]
+
+
+class KvBatch:
+    """A batch of sequences for the calls of ``PagedKV`` (``siso_kv_batch``).  It refers to its tensors: what a program
+    writes into them counts for the calls that follow."""
+
+    def __init__(self, first: torch.Tensor, length: Optional[torch.Tensor], pages: Optional[torch.Tensor], rows: Optional[int],
+                 max_new: int, max_length: int):
+        self.first, self.length, self.pages = first, length, pages
+        self.n = first.shape[0] - 1
+        self.rows = int(first[-1].item()) if rows is None else int(rows)
+        self.tensors = [t for t in (first, length, pages) if t is not None]
+        self._c = _KvBatchStruct(self.n, self.rows, first.data_ptr(), None if length is None else length.data_ptr(),
+                                 None if pages is None else pages.data_ptr(), 0 if pages is None else pages.shape[1], int(max_new),
+                                 int(max_length))
+        self._ref = C.addressof(self._c)
+
+
+class PagedKV:
+    """The paged key/value cache of a target model, its attention and the verification of drafts (``siso_kv.h``).
+    Method names follow the C ABI.  Work goes to the stream that was current when the handle was made, or that of
+    ``set_stream``; a caller on another stream orders the two."""
+
+    def __init__(self, kv_heads: int, head_dim: int, pages: int, page_tokens: int = 64, layers: int = 1, dtype: int = BF16,
+                 device: str = "cuda:0"):
+        self.kv_heads, self.head_dim, self.pages, self.page_tokens = int(kv_heads), int(head_dim), int(pages), int(page_tokens)
+        self.layers, self.dtype, self.device = int(layers), int(dtype), torch.device(device)
+        self._h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            rc = _lib.siso_kv_create(self.layers, self.kv_heads, self.head_dim, self.page_tokens, self.pages, self.dtype,
+                                     C.byref(self._h))
+        if rc != OK:
+            self._h = C.c_void_p()
+            raise SisoError(rc, "siso_kv_create failed")
+        self.set_stream(torch.cuda.current_stream(self.device))
+
+    # ------------------------------------------------------------------ plumbing
+    def _check(self, rc: int) -> int:
+        if rc < 0:
+            raise SisoError(rc, _lib.siso_kv_last_error(self._h).decode())
+        return rc
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            _lib.siso_kv_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def set_stream(self, stream: torch.cuda.Stream) -> None:
+        self._stream = stream
+        self._check(_lib.siso_kv_set_stream(self._h, C.c_void_p(stream.cuda_stream)))
+
+    def _used(self, *tensors: Optional[torch.Tensor]) -> None:
+        """Memory that the handle's stream works on is not given to others before that work is done, where torch's
+        allocator would count by another stream."""
+        if torch.cuda.current_stream(self.device) != self._stream:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self._stream)
+
+    def _heads(self, t: torch.Tensor, rows: int, heads: Optional[int], what: str) -> torch.Tensor:
+        if t.device != self.device or t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != rows or t.shape[2] != self.head_dim or \
+                (heads is not None and t.shape[1] != heads):
+            raise ValueError(f"{what}: expected a [{rows}, {'heads' if heads is None else heads}, {self.head_dim}] torch.bfloat16 "
+                             f"tensor on {self.device}")
+        return t if t.stride(2) == 1 else t.contiguous()
+
+    def _out(self, t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str) -> torch.Tensor:
+        if t is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        if t.device != self.device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{what}: expected a contiguous {list(shape)} {dtype} tensor on {self.device}")
+        return t
+
+    # ---------------------------------------------------------------------- calls
+    def batch(self, first: torch.Tensor, length: Optional[torch.Tensor] = None, pages: Optional[torch.Tensor] = None,
+              rows: Optional[int] = None, max_new: int = 0, max_length: int = 0) -> KvBatch:
+        """Sequences for the calls below: rows ``first[b] .. first[b + 1] - 1`` (int32 [n + 1]) are the newest of the ``length[b]``
+        tokens (int32 [n]) in the pages ``pages[b]`` (int32 [n, width]).  ``rows``: first[n] (None: asked of the GPU)."""
+        for t, name, dims in ((first, "first", 1), (length, "length", 1), (pages, "pages", 2)):
+            if t is not None and (t.device != self.device or t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous()):
+                raise ValueError(f"{name}: expected a contiguous int32 tensor of {dims} dimension(s) on {self.device}")
+        n = first.shape[0] - 1
+        if n < 0 or (length is not None and length.shape[0] != n) or (pages is not None and pages.shape[0] != n) or \
+                (length is None) != (pages is None):
+            raise ValueError("first [n + 1], length [n] and pages [n, width] of one n; length and pages both or neither")
+        return KvBatch(first, length, pages, rows, max_new, max_length)
+
+    def write(self, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, layer: int = 0) -> None:
+        k = self._heads(k, batch.rows, self.kv_heads, "k")
+        v = self._heads(v, batch.rows, self.kv_heads, "v")
+        self._used(k, v, *batch.tensors)
+        self._check(_lib.siso_kv_write(self._h, layer, batch._ref, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                                       v.stride(1)))
+
+    def read(self, batch: KvBatch, layer: int = 0, dtype: torch.dtype = torch.bfloat16, out_k: Optional[torch.Tensor] = None,
+             out_v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """``(k, v)`` [rows, kv_heads, head_dim] as the cache holds them, in bfloat16 or float32."""
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("dtype: torch.bfloat16 or torch.float32")
+        shape = (batch.rows, self.kv_heads, self.head_dim)
+        out_k, out_v = self._out(out_k, shape, dtype, "out_k"), self._out(out_v, shape, dtype, "out_v")
+        self._used(out_k, out_v, *batch.tensors)
+        self._check(_lib.siso_kv_read(self._h, layer, batch._ref, F32 if dtype == torch.float32 else BF16, out_k.data_ptr(),
+                                      out_v.data_ptr()))
+        return out_k, out_v
+
+    def attend(self, batch: KvBatch, q: torch.Tensor, layer: int = 0, scale: Optional[float] = None, window: int = 0,
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, with_lse: bool = False):
+        """Attention of ``q`` [rows, heads, head_dim] (scale: 1 / sqrt(head_dim) unless given): ``out``, or ``(out, lse)`` if ``lse``
+        is given or asked for."""
+        q = self._heads(q, batch.rows, None, "q")
+        shape = tuple(q.shape)
+        out = self._out(out, shape, torch.bfloat16, "out")
+        if with_lse or lse is not None:
+            lse = self._out(lse, shape[:2], torch.float32, "lse")
+        self._used(q, out, lse, *batch.tensors)
+        self._check(_lib.siso_kv_attend(self._h, layer, batch._ref, q.data_ptr(), q.stride(0), q.stride(1), shape[1],
+                                        self.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
+                                        None if lse is None else lse.data_ptr()))
+        return out if lse is None else (out, lse)
+
+    def verify(self, batch: KvBatch, tokens: torch.Tensor, target: torch.Tensor, draft: Optional[torch.Tensor] = None,
+               u_accept: Optional[torch.Tensor] = None, u_sample: Optional[torch.Tensor] = None,
+               out_accepted: Optional[torch.Tensor] = None, out_tokens: Optional[torch.Tensor] = None
+               ) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Which drafted tokens stay, and the token that follows: ``(accepted int32 [n], tokens int32 [rows])``.  ``target`` and
+        ``draft``: [rows, vocab], float32 or bfloat16.  Without random numbers: greedy."""
+        rows, n = batch.rows, batch.n
+        for t, name, dtype, size in ((tokens, "tokens", torch.int32, rows), (u_accept, "u_accept", torch.float32, rows),
+                                     (u_sample, "u_sample", torch.float32, n)):
+            if t is not None and (t.device != self.device or t.dtype != dtype or t.shape != (size,) or not t.is_contiguous()):
+                raise ValueError(f"{name}: expected a contiguous [{size}] {dtype} tensor on {self.device}")
+        if target.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("target: float32 or bfloat16")
+        for t, name in ((target, "target"), (draft, "draft")):
+            if t is not None and (t.device != self.device or t.dtype != target.dtype or t.dim() != 2 or t.shape[0] != rows or
+                                  t.shape[1] != target.shape[1] or t.stride(1) != 1):
+                raise ValueError(f"{name}: expected a [{rows}, vocab] {target.dtype} tensor on {self.device}, entries of a row side by side")
+        out_accepted = self._out(out_accepted, (n,), torch.int32, "out_accepted")
+        out_tokens = self._out(out_tokens, (rows,), torch.int32, "out_tokens")
+        self._used(tokens, target, draft, u_accept, u_sample, out_accepted, out_tokens, *batch.tensors)
+        p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._check(_lib.siso_kv_verify(self._h, batch._ref, tokens.data_ptr(), target.shape[1], F32 if target.dtype == torch.float32 else BF16,
+                                        target.data_ptr(), target.stride(0), p(draft), 0 if draft is None else draft.stride(0),
+                                        p(u_accept), p(u_sample), out_accepted.data_ptr(), out_tokens.data_ptr()))
+        return out_accepted, out_tokens
+
+    def bad_pages(self) -> int:
+        return self._check(_lib.siso_kv_bad_pages(self._h))
