@@ -28,7 +28,7 @@ KvPool kv_pool(const siso_kv *kv, int layer) {
     p.ks = kv->ks ? kv->ks + (size_t)layer * kv->layer_scales : nullptr;
     p.vs = kv->vs ? kv->vs + (size_t)layer * kv->layer_scales : nullptr;
     p.bad = kv->counters;
-    p.pages = kv->pages;
+    p.pages = (int)kv->pages;
     p.kv_heads = kv->kv_heads;
     p.shift = __builtin_ctz(kv->page_tokens);
     p.dim = kv->dim;
@@ -92,10 +92,11 @@ extern "C" int siso_kv_create(int layers, int kv_heads, int head_dim, int page_t
             ok = ok && hipMalloc((void **)&kv->ks, scales) == hipSuccess && hipMalloc((void **)&kv->vs, scales) == hipSuccess;
             ok = ok && hipMemset(kv->ks, 0, scales) == hipSuccess && hipMemset(kv->vs, 0, scales) == hipSuccess;
         }
-        ok = ok && hipMalloc((void **)&kv->counters, 4 * sizeof(u64)) == hipSuccess;
-        ok = ok && hipMemset(kv->counters, 0, 4 * sizeof(u64)) == hipSuccess;
+        const size_t counts = 32 * sizeof(u64) + SISO_KV_WORKGROUPS * sizeof(unsigned);
+        ok = ok && hipMalloc((void **)&kv->counters, counts) == hipSuccess;
+        ok = ok && hipMemset(kv->counters, 0, counts) == hipSuccess;
+        kv->arrived = (unsigned *)(kv->counters + 32);
         ok = ok && hipMalloc((void **)&kv->parts, kv->parts_floats * sizeof(float)) == hipSuccess;
-        ok = ok && hipHostMalloc((void **)&kv->host_pin, sizeof(u64), hipHostMallocDefault) == hipSuccess;
         ok = ok && hipDeviceSynchronize() == hipSuccess;
     }
     if (!ok) {
@@ -116,7 +117,6 @@ extern "C" void siso_kv_destroy(siso_kv *kv) {
     if (kv->vs) (void)hipFree(kv->vs);
     if (kv->counters) (void)hipFree(kv->counters);
     if (kv->parts) (void)hipFree(kv->parts);
-    if (kv->host_pin) (void)hipHostFree(kv->host_pin);
     delete kv;
 }
 
@@ -130,9 +130,10 @@ extern "C" const char *siso_kv_last_error(const siso_kv *kv) { return kv ? kv->e
 
 extern "C" long siso_kv_bad_pages(siso_kv *kv) {
     if (!kv) return SISO_EINVAL;
-    KV_TRY(kv, hipMemcpyAsync(kv->host_pin, kv->counters, sizeof(u64), hipMemcpyDeviceToHost, kv->stream));
+    u64 bad = 0;
+    KV_TRY(kv, hipMemcpyAsync(&bad, kv->counters, sizeof(u64), hipMemcpyDeviceToHost, kv->stream));
     KV_TRY(kv, hipStreamSynchronize(kv->stream));
-    return (long)kv->host_pin[0];
+    return (long)bad;
 }
 
 // ---------------------------------------------------------------------------- writing and reading
@@ -142,7 +143,7 @@ extern "C" long siso_kv_bad_pages(siso_kv *kv) {
 struct KvBlock {
     KvSequence s;
     int at;    // position of the block's first token
-    long page;  // -1: none
+    int page;  // -1: none
 };
 
 // Slots for siso_kv_write and siso_kv_read: m rows stand in at most m / 16 + 2 blocks.
@@ -337,7 +338,7 @@ __global__ __launch_bounds__(256) void k_kv_read(KvPool pool, KvBatch batch, O *
     const int row = blk.at + key - blk.s.start;
     const bool in = row >= 0 && row < blk.s.rows;
     const bool held = blk.page >= 0;
-    const long page = held ? blk.page : 0;
+    const int page = held ? blk.page : 0;
     const char *kb = pool.k + kv_block_at(pool, page, head, blk.at) * ES;
     const char *vb = pool.v + kv_block_at(pool, page, head, blk.at) * ES;
     for (int j = t; j < 2 * dp; j += 256) {

@@ -1,5 +1,6 @@
 // Attention over the paged cache (siso_kv_attend).  Layout of the pages: kv_internal.h.
 #include <math.h>
+#include <type_traits>
 
 #include "kv_internal.h"
 
@@ -16,45 +17,33 @@ struct KvAttend {
     long q_token, q_head;
     int vec;
     int group;         // query heads of a kv head
-    float scale;       // times log2(e): the softmax is one of powers of two
+    float scale;       // its size times log2(e), above zero: the softmax is one of powers of two
+    unsigned negate;   // a scale below zero: the queries' signs are turned
     int window;        // 0 = all
-    int splits, split_len;  // the axis of positions is cut every split_len (a multiple of 32); the last takes what is left
     bf16_t *out;
     float *lse;
-    float *parts;
-    long slot0;
+    float *parts;       // [2 * workgroups]: sums [32][DP], then maximum and sum of each row
+    unsigned *arrived;  // [workgroups]: parts of a tile that are there, by the first workgroup that works on it; zeros between calls
 };
-
-#define KV_TILE_SHIFT 5  // rows of a tile
-#define KV_TILE_EXTRA 1
 
 struct KvTile {
     KvSequence s;
-    int row0, rows;    // of the sequence's rows of work: the first one of the tile, how many there are
-    int lo, hi;        // positions that some row of the tile sees
+    int row0, rows;      // of the sequence's rows of work: the first one of the tile, how many there are
+    int lo, hi;          // positions that some row of the tile sees
     int all_lo, all_hi;  // positions that all rows of the tile see
 };
-
-__device__ __forceinline__ bool kv_find_tile(const KvAttend &a, long slot, KvTile &t) {
-    const int b = a.batch.single && a.group <= 32 ? (int)slot : kv_sequence_of(a.batch, slot, a.group, KV_TILE_SHIFT, KV_TILE_EXTRA);
-    t.s = kv_sequence(a.batch, b);
-    const long j = a.batch.single && a.group <= 32 ? 0 : slot - kv_slots_before(t.s.first, b, a.group, KV_TILE_SHIFT, KV_TILE_EXTRA);
-    const long work = (long)t.s.rows * a.group;
-    if (j < 0 || j * 32 >= work) return false;
-    t.row0 = (int)(j * 32);
-    t.rows = work - j * 32 < 32 ? (int)(work - j * 32) : 32;
-    const int first = t.s.start + t.row0 / a.group, last = t.s.start + (t.row0 + t.rows - 1) / a.group;
-    t.hi = last + 1 > 0 ? last + 1 : 0;
-    t.lo = a.window > 0 && first - a.window + 1 > 0 ? first - a.window + 1 : 0;
-    t.all_hi = first + 1;
-    t.all_lo = a.window > 0 && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
-    return true;
+__device__ __forceinline__ int kv_window_from(const KvAttend &a, int pos) {  // the first position that a row at `pos` sees
+    return a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
 }
-// The part of a tile's positions that split `s` takes: [from, to), from a multiple of 32.
-__device__ __forceinline__ void kv_split(const KvAttend &a, const KvTile &t, int s, int &from, int &to) {
-    from = s * a.split_len;
-    to = s + 1 == a.splits || t.hi < from + a.split_len ? t.hi : from + a.split_len;
-    if (from < (t.lo & ~31)) from = t.lo & ~31;
+__device__ __forceinline__ void kv_tile(const KvAttend &a, int row0, int size, KvTile &t) {
+    const int work = t.s.rows * a.group;  // (at most 2^24 rows, 128 heads: 2^31 at most, and then not here)
+    t.row0 = row0;
+    t.rows = work - row0 < size ? work - row0 : size;
+    const int first = t.s.start + row0 / a.group, last = t.s.start + (row0 + t.rows - 1) / a.group;
+    t.hi = last + 1 > 0 ? last + 1 : 0;
+    t.lo = kv_window_from(a, first);
+    t.all_hi = first + 1;
+    t.all_lo = kv_window_from(a, last);
 }
 
 __device__ __forceinline__ bf16x8_t kv_as_bf16(u32x4_t x) { return __builtin_bit_cast(bf16x8_t, x); }
@@ -81,45 +70,189 @@ __device__ __forceinline__ float kv_both_halves_sum(float v) {
     return p.a + p.b;
 }
 
-// One workgroup for a tile of 32 rows and a split of the positions; its four waves take every fourth 32 of them, each with sums of
-// its own, which are joined through LDS in the order of the waves.  Keys and values go straight from memory to
-// registers: no wave reads what another does.
+#define KV_PART(DP) (32 * ((DP) + 2))
+
+// Parts go from one workgroup to another within a kernel, past the caches of each XCD: single stores and loads at the scope of the
+// device.  A fence of that scope instead writes back and empties the XCD's whole L2, once for each workgroup: with it 64 sequences took 260
+// to 560 us, the more the finer they were split.
+__device__ __forceinline__ void kv_leave(float *at, float a, float b) {
+    __hip_atomic_store((u64 *)at, (u64)__float_as_uint(a) | ((u64)__float_as_uint(b) << 32), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 kv_found(const float *at) {
+    const u64 v = __hip_atomic_load((const u64 *)at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+
+// Four sums of a row and what goes with them, brought from their own maximum to `top`.
+__device__ __forceinline__ void kv_add_part(float mj, float top, float lj, float4 y, float &sum, float4 &x) {
+    const float f = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mj - top);
+    sum += lj * f;
+    x.x += y.x * f, x.y += y.y * f, x.z += y.z * f, x.w += y.w * f;
+}
+__device__ __forceinline__ void kv_finish(const KvAttend &a, const KvTile &t, int head, int r, int d, float top, float sum, float4 x) {
+    const int work = t.row0 + r, tok = work / a.group, hd = head * a.group + work % a.group;
+    const size_t at = (size_t)(t.s.first + tok) * a.group * a.pool.kv_heads + hd;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    if (d < a.pool.dim)
+        *(uint2 *)(a.out + at * a.pool.dim + d) = make_uint2((unsigned)f32_to_bf16(x.x * inv) | ((unsigned)f32_to_bf16(x.y * inv) << 16),
+                                                             (unsigned)f32_to_bf16(x.z * inv) | ((unsigned)f32_to_bf16(x.w * inv) << 16));
+    if (d == 0 && a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f;
+}
+
+// Sequences of few rows of work (at most KV_FEW: one token, a draft's few).  Each has tiles of 32 rows for each of its kv heads, each tile the
+// same number of units of KS positions (32, or 64 of 64 elements); all units of all sequences, one after the other, are cut into as many equal stretches as there are
+// workgroups.  So every workgroup has the same to do, whatever the lengths are, and nobody has to know them beforehand.
+#define KV_FEW 128
+#define KV_LEAST 4  // units of a stretch, at least: one for each wave
+template <int KS>
+struct KvFew {
+    int chunk;            // the first of 64 sequences that this wave holds, one a lane
+    int first, rows, length;  // of this lane's sequence
+    int tiles, range;     // its tiles (of all kv heads; 0: not one of these sequences) and the units of each
+    unsigned upto, mine;  // units before the next sequence, its own
+    __device__ __forceinline__ static int range_of(const KvAttend &a, int start, int length, int &from) {
+        from = kv_window_from(a, start) & ~(KS - 1);
+        const int r = (length - from + KS - 1) / KS;
+        return r > 1 ? r : 1;
+    }
+    __device__ __forceinline__ void load(const KvAttend &a, int b) {
+        tiles = range = first = rows = length = 0;
+        if (b >= a.batch.n) return;
+        const KvSequence s = kv_sequence(a.batch, b);
+        first = s.first;
+        rows = s.rows;
+        length = s.length;
+        if (rows == 0 || rows > KV_FEW || rows * a.group > KV_FEW) return;
+        int from;
+        tiles = ((rows * a.group + 31) >> 5) * a.pool.kv_heads;
+        range = range_of(a, s.start, length, from);
+    }
+    // Units are numbered so that a tile's are a multiple of `whole`.
+    __device__ __forceinline__ void number(const KvAttend &a, unsigned before, int whole) {
+        const int lane = threadIdx.x & 63;
+        mine = tiles * (whole > 1 ? (range + whole - 1) / whole * whole : range);
+        upto = mine;
+        if (a.batch.n > 1)
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const unsigned x = __shfl_up(upto, off);
+                if (lane >= off) upto += x;
+            }
+        else upto = __builtin_amdgcn_readfirstlane(upto);
+        upto += before;
+    }
+    __device__ __forceinline__ unsigned end() const { return __builtin_amdgcn_readlane(upto, 63); }
+    // Where tiles are few, a stretch lies within one of them: so many units that no more than `most` stretches come of it.  Else a
+    // tile may end within a stretch.  Returns all units, sets their number in a stretch and what a tile's are a multiple of.
+    __device__ __forceinline__ unsigned plan(const KvAttend &a, unsigned most, unsigned &stretch, int &whole) {
+        chunk = 0;
+        load(a, threadIdx.x & 63);
+        unsigned all_tiles, all;
+        if (a.batch.n == 1) {
+            all_tiles = __builtin_amdgcn_readfirstlane(tiles);
+            all = all_tiles * __builtin_amdgcn_readfirstlane(range);
+        } else {
+            unsigned t = tiles, u = tiles * range;
+            if (a.batch.n > 64) {
+                KvFew other;
+#pragma unroll 4
+                for (int b = 64 + (threadIdx.x & 63); b < a.batch.n; b += 64) {
+                    other.load(a, b);
+                    t += other.tiles;
+                    u += other.tiles * other.range;
+                }
+            }
+            auto add = [](unsigned x, unsigned y) __attribute__((always_inline)) { return x + y; };
+            all_tiles = __builtin_amdgcn_readfirstlane(wave_fold(t, add));
+            all = __builtin_amdgcn_readfirstlane(wave_fold(u, add));
+        }
+        const bool apart = 2 * all_tiles <= most;
+        const unsigned ways = apart ? most - all_tiles : most;
+        stretch = (all + ways - 1) / ways;
+        if (stretch < KV_LEAST) stretch = KV_LEAST;
+        stretch = __builtin_amdgcn_readfirstlane(stretch);
+        whole = apart ? stretch : 1;
+        number(a, 0, whole);
+        return a.batch.n == 1 ? end() : apart ? most * stretch : all;  // (apart: the stretches beyond the last find nothing)
+    }
+    // The sequence that unit x is of, or -1; `before`: the units before it.
+    __device__ __forceinline__ int find(const KvAttend &a, unsigned x, int whole, unsigned &before, KvSequence &s) {
+        while (end() <= x) {
+            if (chunk + 64 >= a.batch.n) return -1;
+            const unsigned so_far = end();
+            chunk += 64;
+            load(a, chunk + (threadIdx.x & 63));
+            number(a, so_far, whole);
+        }
+        const int at = __ffsll((long long)__ballot(upto > x)) - 1;
+        before = __builtin_amdgcn_readlane(upto - mine, at);
+        s.b = chunk + at;
+        s.first = __builtin_amdgcn_readlane(first, at);
+        s.rows = __builtin_amdgcn_readlane(rows, at);
+        s.length = __builtin_amdgcn_readlane(length, at);
+        s.start = s.length - s.rows;
+        return s.b;
+    }
+};
+// One workgroup for a stretch of units; its four waves take every fourth unit of a tile, each with sums of its own, which are
+// joined through LDS in the order of the waves.  Keys and values go straight from memory to registers: no wave reads what another does.
+// A tile that several workgroups have a part of is finished by the one that is done last, from all parts, in their order.
+// KS: positions of a step.  A wave has one step's operands on their way while it works on the last one's.
+constexpr int kv_step(int dp) { return dp <= 64 ? 64 : 32; }
 template <int DP, bool FP8>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAttend a) {
     constexpr int ES = FP8 ? 1 : 2;
+    constexpr int KS = kv_step(DP), SUBS = KS / 32, BLOCKS = KS / 16;
     constexpr int NF = FP8 ? DP / 32 : DP / 16;  // 16-byte operands of a lane for 32 keys, and for 32 values
     constexpr int NU = DP / 32;
     constexpr int RS = DP + 4;  // floats of a row in LDS
-    __shared__ __attribute__((aligned(16))) float sh[4 * 32 * RS + 2 * 4 * 32];  // sums [4][32][RS], then maxima and sums [2][4][32]
-    float *sh_m = sh + 4 * 32 * RS, *sh_l = sh_m + 4 * 32;
+    __shared__ __attribute__((aligned(16))) float sh[4 * 32 * RS];  // sums of each wave
+    __shared__ float sh_m[4 * 32], sh_l[4 * 32];
+    __shared__ int sh_last;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
-    const int head = blockIdx.x % a.pool.kv_heads;
-    const long item = blockIdx.x / a.pool.kv_heads;
-    const long slot = a.slot0 + item / a.splits;
-    const int split = (int)(item % a.splits);
+    KvFew<KS> few;
+    unsigned stretch;
+    int whole;
+    const unsigned all = few.plan(a, gridDim.x, stretch, whole);
+    unsigned unit = blockIdx.x * stretch;
+    const unsigned last_unit = unit + stretch < all ? unit + stretch : all;
+#pragma unroll 1
+    while (unit < last_unit) {
     KvTile t;
-    if (!kv_find_tile(a, slot, t)) return;
-    int from, to;
-    kv_split(a, t, split, from, to);
-    if (from >= to && a.splits > 1) return;
+    unsigned before;
+    if (few.find(a, unit, whole, before, t.s) < 0) return;
+    int base;
+    int range = KvFew<KS>::range_of(a, t.s.start, t.s.length, base);
+    if (whole > 1) range = (range + whole - 1) / whole * whole;
+    range = __builtin_amdgcn_readfirstlane(range);
+    const int which = __builtin_amdgcn_readfirstlane((unit - before) / (unsigned)range), unit0 = unit - before - which * range;
+    const int units = last_unit - unit < (unsigned)(range - unit0) ? last_unit - unit : range - unit0;
+    const int tile = __builtin_amdgcn_readfirstlane(which / a.pool.kv_heads), head = which - tile * a.pool.kv_heads;
+    kv_tile(a, tile * 32, 32, t);
+    const unsigned tile_unit = unit - unit0;
+    const int first_workgroup = __builtin_amdgcn_readfirstlane(tile_unit / stretch), count = __builtin_amdgcn_readfirstlane((tile_unit + range - 1) / stretch) - first_workgroup + 1;
+    int from = base + KS * unit0, to = from + KS * units;
+    if (from < (t.lo & ~(KS - 1))) from = t.lo & ~(KS - 1);
+    if (to > t.hi) to = t.hi;
 
     // this lane's row (of both halves) as the operand Q^T
     const int row = t.row0 + n, token = row / a.group, qh = head * a.group + row % a.group;
     const bool valid = n < t.rows;
     const int pos = t.s.start + token;
-    bf16x8_t qf[DP / 16];
+    u32x4_t qx[DP / 16];
+    const bf16_t *const q_row = a.q + (long)(t.s.first + (valid ? token : 0)) * a.q_token + (long)(valid ? qh : 0) * a.q_head;
+    auto q_at = [&](int s) { return FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h; };
+    if (a.vec) {
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-        const int d = FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h;
-        u32x4_t x = {0, 0, 0, 0};
-        if (valid && d < a.pool.dim) {
-            const bf16_t *from_q = a.q + (long)(t.s.first + token) * a.q_token + (long)qh * a.q_head + d;
-            if (a.vec) x = *(const u32x4_t *)from_q;
-            else
+        for (int s = 0; s < DP / 16; ++s) qx[s] = *(const u32x4_t *)(q_row + (q_at(s) < a.pool.dim ? q_at(s) : 0));
+    } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = (unsigned)from_q[2 * i] | ((unsigned)from_q[2 * i + 1] << 16);
-        }
-        qf[s] = kv_as_bf16(x);
+        for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bf16_t *two = q_row + (q_at(s) < a.pool.dim ? q_at(s) : 0) + 2 * i;
+                qx[s][i] = (unsigned)two[0] | ((unsigned)two[1] << 16);
+            }
     }
 
     f32x16_t o[NU];
@@ -127,144 +260,174 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
     for (int u = 0; u < NU; ++u) o[u] = f32x16_t{};
     float m = -INFINITY, l = 0.f;
 
-    u32x4_t kf[NF], vf[NF];
-    long page[2], next_page[2];
-    // the pages of the two blocks from `at` on; a block beyond what the tile sees takes the other's
-    auto find_pages = [&](int at, long (&p)[2]) {
-        p[0] = kv_page(a.pool, a.batch, t.s.b, at);
-        p[1] = at + 16 < t.hi ? kv_page(a.pool, a.batch, t.s.b, at + 16) : p[0];
+    u32x4_t kf[SUBS * NF], vf[SUBS * NF];
+    float scales[SUBS];  // (8 bits) of keys, then of values, one a lane
+    int page[BLOCKS], next_page[BLOCKS];
+    // what the table says of the blocks from `at` on; of a block beyond what the tile sees, of the last one
+    auto find_pages = [&](int at, int (&p)[BLOCKS]) {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) p[i] = kv_page_entry(a.pool, a.batch, t.s.b, at + 16 * i < t.hi ? at + 16 * i : t.hi - 1);
     };
-    auto load_keys = [&](int at, const long (&p)[2]) {
-        const int blk = (lane >> 4) & 1;
-        const size_t b0 = kv_block_at(a.pool, p[0] < 0 ? 0 : p[0], head, at), b1 = kv_block_at(a.pool, p[1] < 0 ? 0 : p[1], head, at + 16);
-        const char *base = a.pool.k + (blk ? b1 : b0) * ES + h * 256 + (lane & 15) * 16;
+    auto load_keys = [&](int at, const int (&p)[BLOCKS]) {
 #pragma unroll
-        for (int s = 0; s < NF; ++s) kf[s] = *(const u32x4_t *)(base + s * 512);
-    };
-    auto load_values = [&](int at, const long (&p)[2]) {
+        for (int sub = 0; sub < SUBS; ++sub) {
+            const size_t b0 = kv_block_at(a.pool, kv_is_page(a.pool, p[2 * sub]) ? p[2 * sub] : 0, head, at + 32 * sub),
+                         b1 = kv_block_at(a.pool, kv_is_page(a.pool, p[2 * sub + 1]) ? p[2 * sub + 1] : 0, head, at + 32 * sub + 16);
+            const char *from_k = a.pool.k + ((lane >> 4) & 1 ? b1 : b0) * ES + h * 256 + (lane & 15) * 16;
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-            const char *base = a.pool.v + kv_block_at(a.pool, p[blk] < 0 ? 0 : p[blk], head, at + 16 * blk) * ES + (h * (NF / 2) * 32 + n) * 16;
-#pragma unroll
-            for (int u = 0; u < NF / 2; ++u) vf[blk * (NF / 2) + u] = *(const u32x4_t *)(base + u * 512);
+            for (int s = 0; s < NF; ++s) kf[sub * NF + s] = *(const u32x4_t *)(from_k + s * 512);
         }
-    };
-
-    int at = from + 32 * w;
-    if (at < to) {
-        find_pages(at, page);
-        load_keys(at, page);
-        load_values(at, page);
-    }
-    for (; at < to; at += 128) {
-        const bool more = at + 128 < to;
-        if (more) find_pages(at + 128, next_page);
-        float ks[16], vs[16];
         if constexpr (FP8) {
+            const int key = lane & (KS - 1);
+            size_t from_s = 0;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const size_t sc = kv_scale_at(a.pool, page[g >> 1] < 0 ? 0 : page[g >> 1], head, at + 16 * (g >> 1)) + 8 * (g & 1) + 4 * h;
-                const float4 x = *(const float4 *)(a.pool.ks + sc), y = *(const float4 *)(a.pool.vs + sc);
-                ks[4 * g] = x.x, ks[4 * g + 1] = x.y, ks[4 * g + 2] = x.z, ks[4 * g + 3] = x.w;
-                vs[4 * g] = y.x, vs[4 * g + 1] = y.y, vs[4 * g + 2] = y.z, vs[4 * g + 3] = y.w;
+            for (int i = 0; i < BLOCKS; ++i) {
+                const size_t x = kv_scale_at(a.pool, kv_is_page(a.pool, p[i]) ? p[i] : 0, head, at + 16 * i);
+                from_s = key >> 4 == i ? x : from_s;
+            }
+            from_s += key & 15;
+            if constexpr (SUBS == 1) scales[0] = (h ? a.pool.vs : a.pool.ks)[from_s];
+            else {
+                scales[0] = a.pool.ks[from_s];
+                scales[1] = a.pool.vs[from_s];
             }
         }
-        f32x16_t s = {};
-        if constexpr (FP8) {
+    };
+    auto load_values = [&](int at, const int (&p)[BLOCKS]) {
+#pragma unroll
+        for (int blk = 0; blk < BLOCKS; ++blk) {
+            const char *from_v = a.pool.v + kv_block_at(a.pool, kv_is_page(a.pool, p[blk]) ? p[blk] : 0, head, at + 16 * blk) * ES + (h * (NF / 2) * 32 + n) * 16;
+#pragma unroll
+            for (int u = 0; u < NF / 2; ++u) vf[blk * (NF / 2) + u] = *(const u32x4_t *)(from_v + u * 512);
+        }
+    };
+    float *const sh_scales = sh + w * 32 * RS;  // this wave's: keys' [KS], values' [KS]
+
+    // One step: KS positions from `at` on, while the next ones' keys, then values, are fetched, as soon as their registers are free.
+    // (Whether there are any is known when this is compiled: what is fetched on one way only would be waited for on both.)
+    auto step = [&](int at, auto has_next) __attribute__((always_inline)) {
+        constexpr bool more = decltype(has_next)::value;
+        f32x16_t s[SUBS];
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            s[sub] = f32x16_t{};
 #pragma unroll
             for (int i = 0; i < NF; ++i) {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_codes_bf16(kf[i][0], kf[i][1]), qf[2 * i], s, 0, 0, 0);
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_codes_bf16(kf[i][2], kf[i][3]), qf[2 * i + 1], s, 0, 0, 0);
+                const u32x4_t x = kf[sub * NF + i];
+                if constexpr (FP8) {
+                    s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_codes_bf16(x[0], x[1]), kv_as_bf16(qx[2 * i]), s[sub], 0, 0, 0);
+                    s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_codes_bf16(x[2], x[3]), kv_as_bf16(qx[2 * i + 1]), s[sub], 0, 0, 0);
+                } else s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_as_bf16(x), kv_as_bf16(qx[i]), s[sub], 0, 0, 0);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NF; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_as_bf16(kf[i]), qf[i], s, 0, 0, 0);
         }
-        if (more) load_keys(at + 128, next_page);
+        if constexpr (FP8) {  // a lane has one position's scales and needs those of its registers': through LDS
+#pragma unroll
+            for (int i = 0; i < SUBS; ++i) sh_scales[64 * i + lane] = scales[i];
+#pragma unroll
+            for (int g = 0; g < 4 * SUBS; ++g) {
+                const float4 x = *(const float4 *)(sh_scales + 8 * g + 4 * h);
+                s[g >> 2][4 * (g & 3)] *= x.x;
+                s[g >> 2][4 * (g & 3) + 1] *= x.y;
+                s[g >> 2][4 * (g & 3) + 2] *= x.z;
+                s[g >> 2][4 * (g & 3) + 3] *= x.w;
+            }
+        }
+        if constexpr (more) load_keys(at + 4 * KS, next_page);
 
-        // register r holds position at + 8 (r / 4) + 4 h + r % 4 of this lane's row
-        const bool edge = at + 32 > t.all_hi || at < t.all_lo || (page[0] | page[1]) < 0;
-        unsigned seen = 0xFFFFu;
+        // register r of a 32 holds position 8 (r / 4) + 4 h + r % 4 of this lane's row
+        bool none = false;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= FP8 ? ks[r] * a.scale : a.scale;
+        for (int i = 0; i < BLOCKS; ++i) none = none || !kv_is_page(a.pool, page[i]);
+        const bool edge = at + KS > t.all_hi || at < t.all_lo || none;
+        unsigned seen[SUBS];
         if (edge) {
-            if (lane == 0 && (page[0] | page[1]) < 0) atomicAdd(a.pool.bad, 1ull);
-            seen = 0;
+            if (lane == 0 && none) atomicAdd(a.pool.bad, 1ull);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int p = at + 8 * (r >> 2) + 4 * h + (r & 3);
-                if (p <= pos && (a.window == 0 || p > pos - a.window) && page[r >> 3] >= 0) seen |= 1u << r;
-                s[r] = seen >> r & 1 ? s[r] : -INFINITY;
+            for (int sub = 0; sub < SUBS; ++sub) {
+                seen[sub] = 0;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int p = at + 32 * sub + 8 * (r >> 2) + 4 * h + (r & 3);
+                    if (p <= pos && (a.window == 0 || p > pos - a.window) && kv_is_page(a.pool, page[2 * sub + (r >> 3)])) seen[sub] |= 1u << r;
+                    s[sub][r] = seen[sub] >> r & 1 ? s[sub][r] : -INFINITY;
+                }
             }
         }
-        float top = s[0];
+        float top = s[0][0];
 #pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+        for (int r = 1; r < 16 * SUBS; ++r) top = fmaxf(top, s[r >> 4][r & 15]);
         top = fmaxf(m, kv_both_halves_max(top));
         if (__ballot(top > m) != 0) {  // (a maximum that stays needs no new sums)
-            const float down = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+            const float down = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * a.scale);
             l *= down;
 #pragma unroll
             for (int u = 0; u < NU; ++u) o[u] *= down;
             m = top;
         }
-        const float base = m == -INFINITY ? 0.f : m;
+        const float base = m == -INFINITY ? 0.f : m * a.scale;
         float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(s[r] - base);
-            sum += s[r];
+        for (int r = 0; r < 16 * SUBS; ++r) {
+            s[r >> 4][r & 15] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r >> 4][r & 15], a.scale, -base));
+            sum += s[r >> 4][r & 15];
         }
         l += sum;
         if constexpr (FP8) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] *= vs[r];
+            for (int g = 0; g < 4 * SUBS; ++g) {
+                const float4 x = *(const float4 *)(sh_scales + KS + 8 * g + 4 * h);
+                s[g >> 2][4 * (g & 3)] *= x.x;
+                s[g >> 2][4 * (g & 3) + 1] *= x.y;
+                s[g >> 2][4 * (g & 3) + 2] *= x.z;
+                s[g >> 2][4 * (g & 3) + 3] *= x.w;
+            }
             if (edge)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = seen >> r & 1 ? s[r] : 0.f;  // (the scale there may be NaN)
-        } else if (edge) {
+                for (int r = 0; r < 16 * SUBS; ++r) s[r >> 4][r & 15] = seen[r >> 4] >> (r & 15) & 1 ? s[r >> 4][r & 15] : 0.f;  // (the scale there may be NaN)
+        }
+        bf16x8_t pf[BLOCKS];
+#pragma unroll
+        for (int r = 0; r < 16 * SUBS; ++r) pf[r >> 3][r & 7] = (__bf16)s[r >> 4][r & 15];
+        if (!FP8 && edge) {
             // Nothing times an infinity is NaN: where some rows do not see a position, its value's infinities and NaN are
-            // taken out of the product and added for the rows that see it.
+            // taken out of the product and added, position by position, for the rows that see it.
             bool odd = false;
 #pragma unroll
-            for (int i = 0; i < NF; ++i)
+            for (int i = 0; i < SUBS * NF; ++i)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) odd = odd || kv_not_finite(vf[i][c]);
             if (__ballot(odd) != 0) {
-                float *mine = sh + w * 32 * RS;  // [row][32 positions], this wave's own
 #pragma unroll
-                for (int r = 0; r < 16; ++r) mine[n * 36 + 8 * (r >> 2) + 4 * h + (r & 3)] = seen >> r & 1 ? s[r] : -1.f;
+                for (int blk = 0; blk < BLOCKS; ++blk)
+#pragma unroll 1
+                    for (int slot = 0; slot < 16; ++slot) {  // (the lane half, then the position among its eight)
+                        const unsigned half = slot >> 3 == h ? (slot & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
+                        const u64 seen_by = __ballot(seen[blk >> 1] >> (8 * (blk & 1) + (slot & 7)) & 1);
+                        const bool sees = seen_by >> (n + 32 * (slot >> 3)) & 1;
 #pragma unroll
-                for (int i = 0; i < NF; ++i)
+                        for (int u = 0; u < NU; ++u) {
+                            u32x4_t x;
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const unsigned v = vf[blk * (NF / 2) + u % (NF / 2)][c] & (c == (slot & 7) >> 1 ? half : 0u);
+                                x[c] = kv_not_finite(v) ? v : 0u;
+                            }
+                            const f32x16_t add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_as_bf16(x), pf[blk], f32x16_t{}, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) o[u][r] += sees ? add[r] : 0.f;
+                        }
+                    }
+#pragma unroll
+                for (int i = 0; i < SUBS * NF; ++i)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         if ((vf[i][c] & 0x7F80u) == 0x7F80u) vf[i][c] &= 0xFFFF0000u;
                         if ((vf[i][c] & 0x7F800000u) == 0x7F800000u) vf[i][c] &= 0xFFFFu;
                     }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 1
-                for (int key = 0; key < 32; ++key) {
-                    const long from_page = page[key >> 4];
-                    if (from_page < 0) continue;
-                    const float p = mine[n * 36 + key];
-                    const bf16_t *v = (const bf16_t *)a.pool.v + kv_block_at(a.pool, from_page, head, at + (key & 16)) +
-                                      (size_t)kv_half(key & 15) * DP * 8 + kv_slot(key & 15);
-#pragma unroll
-                    for (int u = 0; u < NU; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const bf16_t x = v[(32 * u + 8 * (r >> 2) + 4 * h + (r & 3)) * 8];
-                            if ((x & 0x7F80u) == 0x7F80u && p >= 0.f) o[u][r] += p * bf16_to_f32(x);
-                        }
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
         }
-        bf16x8_t pf[2];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) pf[r >> 3][r & 7] = (__bf16)s[r];
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
+        for (int blk = 0; blk < BLOCKS; ++blk) {
             if constexpr (FP8) {
 #pragma unroll
                 for (int u = 0; u < NF / 2; ++u) {
@@ -277,16 +440,39 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
                 for (int u = 0; u < NU; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_as_bf16(vf[blk * NU + u]), pf[blk], o[u], 0, 0, 0);
             }
         }
-        if (more) {
-            load_values(at + 128, next_page);
-            page[0] = next_page[0];
-            page[1] = next_page[1];
+        if constexpr (more) {
+            load_values(at + 4 * KS, next_page);
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) page[i] = next_page[i];
         }
+    };
+
+    // Pages are looked up two steps ahead.
+    int at = from + KS * w;
+    if (at < to) {
+        int over_next_page[BLOCKS];
+        find_pages(at, page);
+        find_pages(at + 4 * KS, next_page);
+        load_keys(at, page);
+        load_values(at, page);
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            asm volatile("" : "+v"(qx[i]));  // waited for here, and not at every step along with what has just been asked for
+#pragma unroll
+            for (int c = 0; c < 4; ++c) qx[i][c] = valid && q_at(i) < a.pool.dim ? qx[i][c] ^ a.negate : 0u;
+        }
+        for (; at + 4 * KS < to; at += 4 * KS) {
+            find_pages(at + 8 * KS, over_next_page);
+            step(at, std::true_type());
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) next_page[i] = over_next_page[i];
+        }
+        step(at, std::false_type());
     }
 
     l = kv_both_halves_sum(l);
     if (h == 0) {
-        sh_m[w * 32 + n] = m;
+        sh_m[w * 32 + n] = m * a.scale;
         sh_l[w * 32 + n] = l;
     }
 #pragma unroll
@@ -295,99 +481,518 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
         for (int g = 0; g < 4; ++g)
             *(float4 *)(sh + (w * 32 + n) * RS + 32 * u + 8 * g + 4 * h) = make_float4(o[u][4 * g], o[u][4 * g + 1], o[u][4 * g + 2], o[u][4 * g + 3]);
     __syncthreads();
-    float *part = a.parts + (item * a.pool.kv_heads + head) * (32 * (DP + 2));
-    for (int i = threadIdx.x; i < 32 * (DP / 4); i += 256) {
+    // (of a tile's parts only the first begins with it, and of a workgroup's only one does not)
+    float *part = a.parts + (size_t)(2 * blockIdx.x + (unit0 == 0)) * KV_PART(DP);
+    for (int i = threadIdx.x; i < t.rows * (DP / 4); i += 256) {
         const int r = i / (DP / 4), d = i % (DP / 4) * 4;
-        if (r >= t.rows) break;
-        float top = -INFINITY;
+        float mj[4], top = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = fmaxf(top, sh_m[j * 32 + r]);
+        for (int j = 0; j < 4; ++j) {
+            mj[j] = sh_m[j * 32 + r];
+            top = fmaxf(top, mj[j]);
+        }
         float sum = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float mj = sh_m[j * 32 + r];
-            const float f = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mj - top);
-            sum += sh_l[j * 32 + r] * f;
-            const float4 y = *(const float4 *)(sh + (j * 32 + r) * RS + d);
-            x.x += y.x * f, x.y += y.y * f, x.z += y.z * f, x.w += y.w * f;
+        for (int j = 0; j < 4; ++j) kv_add_part(mj[j], top, sh_l[j * 32 + r], *(const float4 *)(sh + (j * 32 + r) * RS + d), sum, x);
+        if (count <= 1) kv_finish(a, t, head, r, d, top, sum, x);
+        else {
+            kv_leave(part + r * DP + d, x.x, x.y);
+            kv_leave(part + r * DP + d + 2, x.z, x.w);
+            if (d == 0) kv_leave(part + 32 * DP + 2 * r, top, sum);
         }
-        if (a.splits > 1) {
-            *(float4 *)(part + r * DP + d) = x;
-            if (d == 0) {
-                part[32 * DP + 2 * r] = top;
-                part[32 * DP + 2 * r + 1] = sum;
+    }
+    if (count > 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's numbers are where all workgroups see them
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            sh_last = atomicAdd(a.arrived + first_workgroup, 1u) == (unsigned)(count - 1);
+            if (sh_last) a.arrived[first_workgroup] = 0;  // (for the next call: nobody else comes)
+        }
+        __syncthreads();
+        if (sh_last) {
+            const float *parts = a.parts + (size_t)2 * first_workgroup * KV_PART(DP);
+            auto part_of = [&](int s) { return parts + (size_t)(2 * s + (s == 0)) * KV_PART(DP); };
+            // few rows leave threads idle: these take every second, fourth or eighth part
+            const int work = t.rows * (DP / 4), across = work > 128 ? 1 : work > 64 ? 2 : work > 32 ? 4 : 8, wide = 256 / across;
+            const int mine = threadIdx.x & (wide - 1), lead = threadIdx.x / wide;
+            for (int i = mine; i < work || across > 1; i += wide) {
+                const int r = i < work ? i / (DP / 4) : 0, d = i % (DP / 4) * 4;
+                float top = -INFINITY, sum = 0.f;
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int s0 = lead; s0 < count; s0 += 8 * across) {
+                    float2 ml[8], y[8], z[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {  // (all on their way at once; what is beyond the last weighs nothing)
+                        const float *p = part_of(s0 + j * across < count ? s0 + j * across : 0);
+                        ml[j] = kv_found(p + 32 * DP + 2 * r);
+                        y[j] = kv_found(p + r * DP + d);
+                        z[j] = kv_found(p + r * DP + d + 2);
+                    }
+                    float now = top;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (s0 + j * across < count) now = fmaxf(now, ml[j].x);
+                    const float4 had = x;
+                    const float had_sum = sum;
+                    x = make_float4(0.f, 0.f, 0.f, 0.f);
+                    sum = 0.f;
+                    kv_add_part(top, now, had_sum, had, sum, x);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (s0 + j * across < count) kv_add_part(ml[j].x, now, ml[j].y, make_float4(y[j].x, y[j].y, z[j].x, z[j].y), sum, x);
+                    top = now;
+                }
+                if (across > 1) {
+                    *(float4 *)(sh + 8 * threadIdx.x) = x;
+                    *(float2 *)(sh + 8 * threadIdx.x + 4) = make_float2(top, sum);
+                    __syncthreads();
+                    if (lead != 0 || i >= work) break;
+                    for (int j = 1; j < across; ++j) top = fmaxf(top, sh[8 * (j * wide + mine) + 4]);
+                    x = make_float4(0.f, 0.f, 0.f, 0.f);
+                    sum = 0.f;
+                    for (int j = 0; j < across; ++j) {
+                        const float *other = sh + 8 * (j * wide + mine);
+                        kv_add_part(other[4], top, other[5], *(const float4 *)other, sum, x);
+                    }
+                }
+                kv_finish(a, t, head, r, d, top, sum, x);
+                if (across > 1) break;
             }
-            continue;
         }
-        const int work = t.row0 + r, tok = work / a.group, hd = head * a.group + work % a.group;
-        const size_t at_out = (size_t)(t.s.first + tok) * a.group * a.pool.kv_heads + hd;
-        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-        if (d < a.pool.dim)
-            *(uint2 *)(a.out + at_out * a.pool.dim + d) = make_uint2((unsigned)f32_to_bf16(x.x * inv) | ((unsigned)f32_to_bf16(x.y * inv) << 16),
-                                                                    (unsigned)f32_to_bf16(x.z * inv) | ((unsigned)f32_to_bf16(x.w * inv) << 16));
-        if (d == 0 && a.lse) a.lse[at_out] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f;
+    }
+    unit += units;
+    __syncthreads();
     }
 }
 
-// Joins the splits of a tile, in their order.
-template <int DP>
-__global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a) {
-    const int head = blockIdx.x % a.pool.kv_heads;
-    const long slot = blockIdx.x / a.pool.kv_heads;
+// Sequences of more rows of work: a prompt's chunk.  One workgroup for a tile of NW * 32 rows, each wave for 32 of them over all
+// positions.  Keys and values pass through LDS in stages of KEYS positions, three of them: one is used, the next is there, the one
+// after is written while its successor is on its way from memory.  Codes become 16-bit numbers (exactly) on the way in.
+template <int DP, bool FP8>
+struct KvChunk {
+    static constexpr int NW = DP == 128 ? 8 : 4;  // waves: two on each SIMD unit of 128 elements, of 64 three workgroups of one
+    static constexpr int NT = 64 * NW, ROWS = 32 * NW, PER_SIMD = DP == 64 ? 3 : NW / 4;
+    static constexpr int KEYS = DP <= 192 ? 64 : 32, SUBS = KEYS / 32, BLOCKS = KEYS / 16;
+    static constexpr int ES = FP8 ? 1 : 2;
+    static constexpr int NS = DP / 16, NU = DP / 32;
+    static constexpr int BLOCK_CHUNKS = DP * ES;           // 16-byte chunks of a block of 16 positions in memory
+    static constexpr int CHUNKS = BLOCKS * BLOCK_CHUNKS;   // of a stage's keys
+    static constexpr int NL = (CHUNKS + NT - 1) / NT;      // of a thread
+    static constexpr int HALF = KEYS * DP * 2;             // bytes of a stage's keys in LDS
+    static constexpr int STAGE = 2 * HALF + (FP8 ? 2 * KEYS * 4 : 0);
+    static constexpr int LDS = 3 * STAGE;
+    static_assert(LDS <= 160 * 1024, "fits LDS");
+};
+#define KV_CHUNK_PART(ROWS, DP) ((size_t)(ROWS) * ((DP) + 2))
+
+struct KvPieces {
+    long slots, slot0;
+    int ways;  // a tile's positions are cut into at most so many pieces
+    int few;   // sequences of at most so many rows of work are left to k_kv_attend_few
+};
+#define KV_PIECE_LEAST 256  // positions
+// The tile of a slot, of `rows` rows of work, and how its positions are cut: pieces of `per` blocks of KEYS positions from `from` on.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces &p, long slot, KvTile &t, int &from, int &blocks, int &per, int &pieces) {
+    constexpr int SHIFT = ROWS == 256 ? 8 : 7;
+    static_assert(ROWS == 1 << SHIFT, "rows of a tile");
+    const int b = kv_sequence_of(a.batch, slot, a.group, SHIFT, 1);
+    t.s = kv_sequence(a.batch, b);
+    const long j = slot - kv_slots_before(t.s.first, b, a.group, SHIFT, 1), work = (long)t.s.rows * a.group;
+    if (j < 0 || j * ROWS >= work || work <= p.few) return false;
+    kv_tile(a, (int)(j * ROWS), ROWS, t);
+    from = t.lo & ~(KEYS - 1);
+    blocks = t.hi > from ? (t.hi - from + KEYS - 1) / KEYS : 0;
+    per = (blocks + p.ways - 1) / p.ways;
+    if (per < KV_PIECE_LEAST / KEYS) per = KV_PIECE_LEAST / KEYS;
+    pieces = blocks > 0 ? (blocks + per - 1) / per : 1;
+    return true;
+}
+
+template <int DP, bool FP8>
+__global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD)) void k_kv_attend_chunk(KvAttend a, KvPieces p) {
+    using C = KvChunk<DP, FP8>;
+    constexpr int KEYS = C::KEYS, SUBS = C::SUBS, BLOCKS = C::BLOCKS, NS = C::NS, NU = C::NU, NL = C::NL;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
+    // (the tiles of one kv head follow each other at a distance of kv_heads, those that see most first)
+    const int head = blockIdx.x % a.pool.kv_heads, piece = blockIdx.x / a.pool.kv_heads % p.ways;
+    const long slot = p.slot0 + p.slots - 1 - blockIdx.x / (a.pool.kv_heads * p.ways);
     KvTile t;
-    if (!kv_find_tile(a, a.slot0 + slot, t)) return;
-    for (int i = threadIdx.x; i < t.rows * (DP / 4); i += 256) {
+    int from, blocks, per, pieces;
+    if (!kv_chunk_tile<C::ROWS, KEYS>(a, p, slot, t, from, blocks, per, pieces) || piece >= pieces) return;
+    const int first = from + piece * per * KEYS, stages = blocks - piece * per < per ? blocks - piece * per : per;
+
+    // this wave's rows; `any`: there are some
+    const bool any = w * 32 < t.rows;
+    KvTile mine;
+    mine.s = t.s;
+    kv_tile(a, any ? t.row0 + w * 32 : t.row0, 32, mine);
+    const int row = t.row0 + w * 32 + n;
+    const bool valid = row < t.row0 + t.rows;
+    const int token = valid ? row / a.group : 0, qh = head * a.group + (valid ? row % a.group : 0), pos = t.s.start + token;
+    auto q_at = [&](int s) { return FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h; };
+    u32x4_t qx[NS];
+    {
+        const bf16_t *q_row = a.q + (long)(t.s.first + token) * a.q_token + (long)qh * a.q_head;
+        if (a.vec) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) qx[s] = *(const u32x4_t *)(q_row + (q_at(s) < a.pool.dim ? q_at(s) : 0));
+        } else {
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bf16_t *two = q_row + (q_at(s) < a.pool.dim ? q_at(s) : 0) + 2 * i;
+                    qx[s][i] = (unsigned)two[0] | ((unsigned)two[1] << 16);
+                }
+        }
+    }
+    f32x16_t o[NU];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) o[u] = f32x16_t{};
+
+    // ---- stages: pages from the table, a stage from memory to registers, from registers to LDS
+    u32x4_t gk[NL], gv[NL];
+    float gs = 0.f;
+    int entry[BLOCKS];  // what the table says of the stage that is fetched next
+    auto look_up = [&](int at) {
+#pragma unroll
+        for (int blk = 0; blk < BLOCKS; ++blk) entry[blk] = kv_page_entry(a.pool, a.batch, t.s.b, at + 16 * blk < t.hi ? at + 16 * blk : t.hi - 1);
+    };
+    auto fetch = [&](int at) {  // returns a bit for each block that has a page
+        size_t base[BLOCKS];
+        int page[BLOCKS], is_page = 0;
+#pragma unroll
+        for (int blk = 0; blk < BLOCKS; ++blk) {
+            is_page |= kv_is_page(a.pool, entry[blk]) ? 1 << blk : 0;
+            page[blk] = kv_is_page(a.pool, entry[blk]) ? entry[blk] : 0;
+            base[blk] = kv_block_at(a.pool, page[blk], head, at + 16 * blk) * C::ES;
+        }
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int c = threadIdx.x + C::NT * i, blk = c / C::BLOCK_CHUNKS;
+            size_t off = base[0];
+#pragma unroll
+            for (int k = 1; k < BLOCKS; ++k) off = blk == k ? base[k] : off;
+            off += (size_t)(c % C::BLOCK_CHUNKS) * 16;
+            if (C::CHUNKS % C::NT == 0 || c < C::CHUNKS) {
+                gk[i] = *(const u32x4_t *)(a.pool.k + off);
+                gv[i] = *(const u32x4_t *)(a.pool.v + off);
+            }
+        }
+        if (FP8 && threadIdx.x < 2 * KEYS) {
+            const int key = threadIdx.x & (KEYS - 1);
+            int pg = page[0];
+#pragma unroll
+            for (int k = 1; k < BLOCKS; ++k) pg = key >> 4 == k ? page[k] : pg;
+            const float *scales = threadIdx.x < KEYS ? a.pool.ks : a.pool.vs;
+            gs = scales[kv_scale_at(a.pool, pg, head, at + (key & ~15)) + (key & 15)];
+        }
+        return is_page;
+    };
+    auto put = [&](int buffer) {
+        char *to = lds + buffer * C::STAGE;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int c = threadIdx.x + C::NT * i, blk = c / C::BLOCK_CHUNKS, r = c % C::BLOCK_CHUNKS;
+            if (!(C::CHUNKS % C::NT == 0 || c < C::CHUNKS)) continue;
+            if constexpr (FP8) {
+                // K: chunk (2 t + h) of 16 codes and a token; two operands of 8.  V: [h][dimension / 64][32] of two operands.
+                const int kc = r >> 4, key = r & 15, vh = r / (DP / 2), vu = r % (DP / 2) >> 5, vm = r & 31;
+                const int even = 2 * (2 * (kc >> 1)) + (kc & 1);
+                *(bf16x8_t *)(to + blk * 32 * DP + (even * 16 + key) * 16) = kv_codes_bf16(gk[i][0], gk[i][1]);
+                *(bf16x8_t *)(to + blk * 32 * DP + ((even + 2) * 16 + key) * 16) = kv_codes_bf16(gk[i][2], gk[i][3]);
+                *(bf16x8_t *)(to + C::HALF + blk * 32 * DP + (vh * DP + 64 * vu + vm) * 16) = kv_codes_bf16(gv[i][0], gv[i][1]);
+                *(bf16x8_t *)(to + C::HALF + blk * 32 * DP + (vh * DP + 64 * vu + 32 + vm) * 16) = kv_codes_bf16(gv[i][2], gv[i][3]);
+            } else {
+                *(u32x4_t *)(to + c * 16) = gk[i];
+                *(u32x4_t *)(to + C::HALF + c * 16) = gv[i];
+            }
+        }
+        if (FP8 && threadIdx.x < 2 * KEYS) *(float *)(to + 2 * C::HALF + threadIdx.x * 4) = gs;
+    };
+
+    // ---- a stage's work
+    auto scaled = [&](const char *scales, f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
+        if constexpr (FP8)
+#pragma unroll
+            for (int g = 0; g < 4 * SUBS; ++g) {
+                const float4 x = *(const float4 *)(scales + (8 * g + 4 * h) * 4);
+                s[g >> 2][4 * (g & 3)] *= x.x;
+                s[g >> 2][4 * (g & 3) + 1] *= x.y;
+                s[g >> 2][4 * (g & 3) + 2] *= x.z;
+                s[g >> 2][4 * (g & 3) + 3] *= x.w;
+            }
+    };
+    auto scores = [&](const char *stage, f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
+        const char *k = stage + (lane >> 4 & 1) * 32 * DP + h * 256 + (lane & 15) * 16;
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            s[sub] = f32x16_t{};
+            __builtin_amdgcn_sched_barrier(0);  // (operands of one 32 at a time: more do not fit)
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+                s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t *)(k + sub * 64 * DP + i * 512), kv_as_bf16(qx[i]), s[sub], 0, 0, 0);
+        }
+        scaled(stage + 2 * C::HALF, s);
+    };
+    // A maximum that grows by less than 2^8 stays as it is: powers up to 2^8 lose nothing, and the sums need not be brought down.
+    auto powers = [&](f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        float top = s[0][0];
+#pragma unroll
+        for (int r = 1; r < 16 * SUBS; ++r) top = fmaxf(top, s[r >> 4][r & 15]);
+        top = kv_both_halves_max(top);
+        if (__ballot((top - m) * a.scale > 8.f) != 0) {
+            const float now = fmaxf(m, top), down = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - now) * a.scale);
+            l *= down;
+#pragma unroll
+            for (int u = 0; u < NU; ++u) o[u] *= down;
+            m = now;
+        }
+        const float base = m == -INFINITY ? 0.f : m * a.scale;
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16 * SUBS; ++r) {
+            s[r >> 4][r & 15] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r >> 4][r & 15], a.scale, -base));
+            sum += s[r >> 4][r & 15];
+        }
+        l += sum;
+    };
+    auto values_at = [&](const char *stage, int blk, int u) { return stage + C::HALF + blk * 32 * DP + (h * DP + 32 * u + n) * 16; };
+    auto step = [&](const char *stage) __attribute__((always_inline)) {
+        f32x16_t s[SUBS];
+        scores(stage, s);
+        powers(s);
+        scaled(stage + 2 * C::HALF + KEYS * 4, s);
+#pragma unroll
+        for (int blk = 0; blk < BLOCKS; ++blk) {
+            if (blk % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            bf16x8_t pf;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) pf[r] = (__bf16)s[blk >> 1][8 * (blk & 1) + r];
+#pragma unroll
+            for (int u = 0; u < NU; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t *)values_at(stage, blk, u), pf, o[u], 0, 0, 0);
+        }
+    };
+    // The same where some rows do not see all positions, or infinities may stand where nobody sees them (see k_kv_attend_few).
+    auto step_edge = [&](const char *stage, int at, int is_page) __attribute__((always_inline)) {
+        f32x16_t s[SUBS];
+        unsigned seen[SUBS];
+        scores(stage, s);
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            seen[sub] = 0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int p = at + 32 * sub + 8 * (r >> 2) + 4 * h + (r & 3);
+                if (p <= pos && (a.window == 0 || p > pos - a.window) && (is_page >> (2 * sub + (r >> 3)) & 1)) seen[sub] |= 1u << r;
+                s[sub][r] = seen[sub] >> r & 1 ? s[sub][r] : -INFINITY;
+            }
+        }
+        powers(s);
+        scaled(stage + 2 * C::HALF + KEYS * 4, s);
+        if constexpr (FP8)
+#pragma unroll
+            for (int r = 0; r < 16 * SUBS; ++r) s[r >> 4][r & 15] = seen[r >> 4] >> (r & 15) & 1 ? s[r >> 4][r & 15] : 0.f;
+#pragma unroll
+        for (int blk = 0; blk < BLOCKS; ++blk) {
+            __builtin_amdgcn_sched_barrier(0);
+            bf16x8_t pf;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) pf[r] = (__bf16)s[blk >> 1][8 * (blk & 1) + r];
+            bool odd = false;
+            if constexpr (!FP8)
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    const u32x4_t x = *(const u32x4_t *)values_at(stage, blk, u);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) odd = odd || kv_not_finite(x[c]);
+                }
+            if (__ballot(odd) != 0) {
+#pragma unroll 1
+                for (int slot = 0; slot < 16; ++slot) {
+                    const unsigned half = slot >> 3 == h ? (slot & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
+                    const u64 seen_by = __ballot(seen[blk >> 1] >> (8 * (blk & 1) + (slot & 7)) & 1);
+                    const bool sees = seen_by >> (n + 32 * (slot >> 3)) & 1;
+#pragma unroll
+                    for (int u = 0; u < NU; ++u) {
+                        u32x4_t x = *(const u32x4_t *)values_at(stage, blk, u);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            x[c] &= c == (slot & 7) >> 1 ? half : 0u;
+                            x[c] = kv_not_finite(x[c]) ? x[c] : 0u;
+                        }
+                        const f32x16_t add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_as_bf16(x), pf, f32x16_t{}, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[u][r] += sees ? add[r] : 0.f;
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                u32x4_t x = *(const u32x4_t *)values_at(stage, blk, u);
+                if constexpr (!FP8)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if ((x[c] & 0x7F80u) == 0x7F80u) x[c] &= 0xFFFF0000u;
+                        if ((x[c] & 0x7F800000u) == 0x7F800000u) x[c] &= 0xFFFFu;
+                    }
+                o[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_as_bf16(x), pf, o[u], 0, 0, 0);
+            }
+        }
+    };
+
+    if (stages > 0) {
+        int is_page, next_is_page = 0, over_next_is_page = 0;
+        look_up(first);
+        is_page = fetch(first);
+        look_up(first + KEYS);
+        put(0);
+        if (stages > 1) next_is_page = fetch(first + KEYS);
+        look_up(first + 2 * KEYS);
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) qx[i][c] = valid && q_at(i) < a.pool.dim ? qx[i][c] ^ a.negate : 0u;
+        int buffer = 0, next_buffer = 1;
+#pragma unroll 1
+        for (int stage = 0; stage < stages; ++stage) {
+            const int at = first + stage * KEYS;
+            if (stage + 1 < stages) {
+                put(next_buffer);
+                if (stage + 2 < stages) over_next_is_page = fetch(at + 2 * KEYS);
+                look_up(at + 3 * KEYS);
+            }
+            __syncthreads();  // this stage is there; nobody is at work on the one before the last any more
+            if (is_page != (1 << BLOCKS) - 1 && threadIdx.x == 0) atomicAdd(a.pool.bad, 1ull);
+            const char *here = lds + buffer * C::STAGE;
+            if (any && at < mine.hi && at + KEYS > mine.lo) {
+                if (at + KEYS > mine.all_hi || at < mine.all_lo || is_page != (1 << BLOCKS) - 1) step_edge(here, at, is_page);
+                else step(here);
+            }
+            buffer = next_buffer;
+            next_buffer = next_buffer == 2 ? 0 : next_buffer + 1;
+            is_page = next_is_page;
+            next_is_page = over_next_is_page;
+        }
+    }
+    if (!any) return;
+
+    const int r = w * 32 + n;  // of the tile
+    const float sum = kv_both_halves_sum(l), top = m * a.scale;
+    if (pieces > 1) {
+        float *part = a.parts + (size_t)blockIdx.x * KV_CHUNK_PART(C::ROWS, DP);
+        if (!valid) return;
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(float4 *)(part + r * DP + 32 * u + 8 * g + 4 * h) = make_float4(o[u][4 * g], o[u][4 * g + 1], o[u][4 * g + 2], o[u][4 * g + 3]);
+        if (h == 0) *(float2 *)(part + C::ROWS * DP + 2 * r) = make_float2(top, sum);
+        return;
+    }
+    const size_t at_out = (size_t)(t.s.first + token) * a.group * a.pool.kv_heads + qh;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    // the halves change places: each lane has eight elements side by side
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            unsigned x[2], y[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[i] = (unsigned)f32_to_bf16(o[u][8 * k + 2 * i] * inv) | ((unsigned)f32_to_bf16(o[u][8 * k + 2 * i + 1] * inv) << 16);
+                y[i] = (unsigned)f32_to_bf16(o[u][8 * k + 4 + 2 * i] * inv) | ((unsigned)f32_to_bf16(o[u][8 * k + 4 + 2 * i + 1] * inv) << 16);
+            }
+            const auto p0 = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false), p1 = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
+            const int d = 32 * u + 16 * k + 8 * h;
+            if (valid && d < a.pool.dim) *(u32x4_t *)(a.out + at_out * a.pool.dim + d) = u32x4_t{p0[0], p1[0], p0[1], p1[1]};
+        }
+    if (valid && h == 0 && a.lse) a.lse[at_out] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f;
+}
+
+// Joins the pieces of the tiles that were cut, in their order: eight workgroups for a tile.
+template <int DP, bool FP8>
+__global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) {
+    using C = KvChunk<DP, FP8>;
+    const int head = blockIdx.x % a.pool.kv_heads;
+    const long at_slot = blockIdx.x / a.pool.kv_heads;
+    KvTile t;
+    int from, blocks, per, pieces;
+    if (!kv_chunk_tile<C::ROWS, C::KEYS>(a, p, p.slot0 + p.slots - 1 - at_slot, t, from, blocks, per, pieces) || pieces <= 1) return;
+    const float *parts = a.parts + (size_t)(at_slot * p.ways * a.pool.kv_heads + head) * KV_CHUNK_PART(C::ROWS, DP);
+    const size_t next = (size_t)a.pool.kv_heads * KV_CHUNK_PART(C::ROWS, DP);
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < t.rows * (DP / 4); i += 256 * gridDim.y) {
         const int r = i / (DP / 4), d = i % (DP / 4) * 4;
         float top = -INFINITY, sum = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = 0; s < a.splits; ++s) {
-            int from, to;
-            kv_split(a, t, s, from, to);
-            if (from >= to) continue;
-            const float *part = a.parts + ((slot * a.splits + s) * a.pool.kv_heads + head) * (32 * (DP + 2));
-            const float mj = part[32 * DP + 2 * r], lj = part[32 * DP + 2 * r + 1];
-            const float4 y = *(const float4 *)(part + r * DP + d);
-            const float both = fmaxf(top, mj);
-            const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - both), g = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mj - both);
-            x.x = x.x * f + y.x * g, x.y = x.y * f + y.y * g, x.z = x.z * f + y.z * g, x.w = x.w * f + y.w * g;
-            sum = sum * f + lj * g;
-            top = both;
+#pragma unroll 4
+        for (int s = 0; s < pieces; ++s) top = fmaxf(top, parts[s * next + C::ROWS * DP + 2 * r]);
+#pragma unroll 4
+        for (int s = 0; s < pieces; ++s) {
+            const float2 ml = *(const float2 *)(parts + s * next + C::ROWS * DP + 2 * r);
+            kv_add_part(ml.x, top, ml.y, *(const float4 *)(parts + s * next + r * DP + d), sum, x);
         }
-        const int work = t.row0 + r, tok = work / a.group, hd = head * a.group + work % a.group;
-        const size_t at_out = (size_t)(t.s.first + tok) * a.group * a.pool.kv_heads + hd;
-        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-        if (d < a.pool.dim)
-            *(uint2 *)(a.out + at_out * a.pool.dim + d) = make_uint2((unsigned)f32_to_bf16(x.x * inv) | ((unsigned)f32_to_bf16(x.y * inv) << 16),
-                                                                    (unsigned)f32_to_bf16(x.z * inv) | ((unsigned)f32_to_bf16(x.w * inv) << 16));
-        if (d == 0 && a.lse) a.lse[at_out] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f;
+        kv_finish(a, t, head, r, d, top, sum, x);
     }
 }
 
-// Positions of a split, at least: eight tiles of 32 for each of the four waves cost more to join than they gain when cut further.
-#define KV_SPLIT_LEAST 256
-#define KV_WORKGROUPS 1024  // what fills the chip: 256 compute units, two workgroups each, twice
+// Workgroups that run at once: two on each of 256 compute units, one where a wave needs more than half of the registers.
+static int kv_few_workgroups(int dp) { return dp <= 128 ? 512 : 256; }
+static int kv_chunk_workgroups(int dp) { return dp == 64 ? 768 : 256; }
 
 template <int DP, bool FP8>
-static int attend(siso_kv *kv, KvAttend &a, long max_length) {
-    const long slots = a.batch.single && a.group <= 32 ? a.batch.n : kv_slots_before(a.batch.rows, a.batch.n, a.group, KV_TILE_SHIFT, KV_TILE_EXTRA);
-    const long tiles = slots * kv->kv_heads, room = (long)(kv->parts_floats / (32 * (DP + 2)));
-    long splits = (max_length + KV_SPLIT_LEAST - 1) / KV_SPLIT_LEAST;
-    if (splits > KV_WORKGROUPS / tiles) splits = KV_WORKGROUPS / tiles;
-    if (splits > room / tiles) splits = room / tiles;
-    if (splits < 1) splits = 1;
-    a.split_len = (int)((max_length + splits * 128 - 1) / (splits * 128) * 128);
-    if (a.split_len < 128) a.split_len = 128;
-    a.splits = (int)splits;
-    const long piece = (1L << 23) / (kv->kv_heads * splits);  // (a launch has fewer than 2^32 threads)
-    for (a.slot0 = 0; a.slot0 < slots; a.slot0 += piece) {
-        const long now = slots - a.slot0 < piece ? slots - a.slot0 : piece;
-        hipLaunchKernelGGL((k_kv_attend_few<DP, FP8>), dim3((unsigned)(now * splits * kv->kv_heads)), dim3(256), 0, kv->stream, a);
+static int attend_chunks(siso_kv *kv, KvAttend &a, int few) {
+    using C = KvChunk<DP, FP8>;
+    KvPieces p;
+    p.few = few;
+    p.slots = kv_slots_before(a.batch.rows, a.batch.n, a.group, C::ROWS == 256 ? 8 : 7, 1);
+    const long tiles = p.slots * kv->kv_heads, room = (long)(kv->parts_floats / KV_CHUNK_PART(C::ROWS, DP));
+    long ways = tiles <= kv_chunk_workgroups(DP) / 2 ? kv_chunk_workgroups(DP) / tiles : 1;
+    if (ways > room / tiles) ways = room / tiles;
+    if (ways > 64) ways = 64;
+    if (ways < 1) ways = 1;
+    p.ways = (int)ways;
+    if (C::LDS > 64 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_attend_chunk<DP, FP8>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS));
+    const long slots = p.slots, piece = (1L << 23) / (kv->kv_heads * ways);  // (a launch has fewer than 2^32 threads)
+    for (p.slot0 = 0; p.slot0 < slots; p.slot0 += piece) {
+        p.slots = slots - p.slot0 < piece ? slots - p.slot0 : piece;
+        hipLaunchKernelGGL((k_kv_attend_chunk<DP, FP8>), dim3((unsigned)(p.slots * ways * kv->kv_heads)), dim3(C::NT), C::LDS, kv->stream, a, p);
         KV_TRY(kv, hipGetLastError());
-        if (splits > 1) {
-            hipLaunchKernelGGL(k_kv_attend_join<DP>, dim3((unsigned)(now * kv->kv_heads)), dim3(256), 0, kv->stream, a);
+        if (ways > 1) {
+            hipLaunchKernelGGL((k_kv_attend_join<DP, FP8>), dim3((unsigned)(p.slots * kv->kv_heads), 8), dim3(256), 0, kv->stream, a, p);
             KV_TRY(kv, hipGetLastError());
         }
+    }
+    return SISO_OK;
+}
+
+template <int DP, bool FP8>
+static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
+    // Which sequences there are is known on the device only: where both kinds can be, both kernels are launched, and each leaves the other's.
+    if (max_new * a.group > KV_FEW) {
+        const int rc = attend_chunks<DP, FP8>(kv, a, KV_FEW);
+        if (rc != SISO_OK || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
+    }
+    constexpr int KS = kv_step(DP);
+    const long tiles = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads, units = tiles * (max_length / KS + 2);
+    const long enough = (units + KV_LEAST - 1) / KV_LEAST;
+    const dim3 grid((unsigned)(enough < kv_few_workgroups(DP) ? enough : kv_few_workgroups(DP)));
+    // (a launch counts its units in 32 bits: sequences that could have more go in several)
+    const long most = (long)(KV_FEW / 32) * kv->kv_heads * (a.batch.most / KS + 2), step = (1L << 30) / most;
+    if (step < 1) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: %d kv heads of sequences of %d tokens", kv->kv_heads, a.batch.most);
+    const int n = a.batch.n;
+    for (long b0 = 0; b0 < n; b0 += step) {
+        a.batch.n = (int)(n - b0 < step ? n - b0 : step);
+        hipLaunchKernelGGL((k_kv_attend_few<DP, FP8>), grid, dim3(256), 0, kv->stream, a);
+        KV_TRY(kv, hipGetLastError());
+        a.batch.first += a.batch.n;
+        a.batch.length += a.batch.n;
+        a.batch.pages += a.batch.n * a.batch.width;
     }
     return SISO_OK;
 }
@@ -411,20 +1016,24 @@ extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch
     a.q_head = q_head;
     a.vec = ((uintptr_t)q & 15) == 0 && q_token % 8 == 0 && q_head % 8 == 0;
     a.group = heads / kv->kv_heads;
-    a.scale = scale * 1.44269504089f;
+    // (zero as the smallest number: a score of minus infinity times it stays one)
+    a.scale = fmaxf(fabsf(scale) * 1.44269504089f, 1.17549435e-38f);
+    a.negate = scale < 0.f ? 0x80008000u : 0u;
     a.window = window;
     a.out = (bf16_t *)out;
     a.lse = lse;
     a.parts = kv->parts;
+    a.arrived = kv->arrived;
+    const long max_new = batch->max_new > 0 && batch->max_new < a.batch.rows ? batch->max_new : a.batch.rows;
     const long max_length = batch->max_length > 0 && batch->max_length < a.batch.most ? batch->max_length : a.batch.most;
     switch (kv->dp / 64 + (kv->dtype == SISO_FP8 ? 4 : 0)) {
-        case 1: return attend<64, false>(kv, a, max_length);
-        case 2: return attend<128, false>(kv, a, max_length);
-        case 3: return attend<192, false>(kv, a, max_length);
-        case 4: return attend<256, false>(kv, a, max_length);
-        case 5: return attend<64, true>(kv, a, max_length);
-        case 6: return attend<128, true>(kv, a, max_length);
-        case 7: return attend<192, true>(kv, a, max_length);
-        default: return attend<256, true>(kv, a, max_length);
+        case 1: return attend<64, false>(kv, a, max_length, max_new);
+        case 2: return attend<128, false>(kv, a, max_length, max_new);
+        case 3: return attend<192, false>(kv, a, max_length, max_new);
+        case 4: return attend<256, false>(kv, a, max_length, max_new);
+        case 5: return attend<64, true>(kv, a, max_length, max_new);
+        case 6: return attend<128, true>(kv, a, max_length, max_new);
+        case 7: return attend<192, true>(kv, a, max_length, max_new);
+        default: return attend<256, true>(kv, a, max_length, max_new);
     }
 }

@@ -22,7 +22,7 @@ struct KvPool {
     char *k, *v;
     float *ks, *vs;  // NULL: 16 bits
     u64 *bad;
-    long pages;
+    int pages;
     int kv_heads, shift;  // page_tokens = 1 << shift
     int dim, dp;
 };
@@ -74,19 +74,26 @@ __device__ __forceinline__ int kv_sequence_of(const KvBatch &batch, long slot, i
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// The page of position `at` (below most, the same in every lane), or -1.
-__device__ __forceinline__ long kv_page(const KvPool &pool, const KvBatch &batch, int b, int at) {
-    const int page = __builtin_amdgcn_readfirstlane(batch.pages[(long)b * batch.width + (at >> pool.shift)]);
-    return (unsigned)page < (unsigned long)pool.pages ? page : -1;
+// What the table says of position `at` (below most, the same in every lane): by a load of the scalar unit, which no vector load
+// waits for or is waited for with.
+__device__ __forceinline__ int kv_page_entry(const KvPool &pool, const KvBatch &batch, int b, int at) {
+    return *(const __attribute__((address_space(4))) int *)(batch.pages + ((long)b * batch.width + (at >> pool.shift)));
+}
+__device__ __forceinline__ bool kv_is_page(const KvPool &pool, int page) { return (unsigned)page < (unsigned)pool.pages; }
+__device__ __forceinline__ int kv_page(const KvPool &pool, const KvBatch &batch, int b, int at) {  // -1: none
+    const int page = kv_page_entry(pool, batch, b, at);
+    return kv_is_page(pool, page) ? page : -1;
 }
 // Where the block of position `at` of a kv head begins, in bytes for elements of one byte (16 bits: twice that).
-__device__ __forceinline__ size_t kv_block_at(const KvPool &pool, long page, int head, int at) {
-    return ((size_t)(page * pool.kv_heads + head) << pool.shift) * pool.dp + (size_t)(((at & ((1 << pool.shift) - 1)) >> 4) * SISO_KV_BLOCK) * pool.dp;
+__device__ __forceinline__ size_t kv_block_at(const KvPool &pool, int page, int head, int at) {
+    return ((size_t)((long)page * pool.kv_heads + head) << pool.shift) * pool.dp + (size_t)(((at & ((1 << pool.shift) - 1)) >> 4) * SISO_KV_BLOCK) * pool.dp;
 }
-__device__ __forceinline__ size_t kv_scale_at(const KvPool &pool, long page, int head, int at) {
-    return ((size_t)(page * pool.kv_heads + head) << pool.shift) + (at & ((1 << pool.shift) - 1));
+__device__ __forceinline__ size_t kv_scale_at(const KvPool &pool, int page, int head, int at) {
+    return ((size_t)((long)page * pool.kv_heads + head) << pool.shift) + (at & ((1 << pool.shift) - 1));
 }
 #endif
+
+#define SISO_KV_WORKGROUPS 512  // of a launch that leaves parts to be joined, at most
 
 struct siso_kv {
     int layers, kv_heads, dim, dp, page_tokens, dtype;
@@ -95,8 +102,8 @@ struct siso_kv {
     char *k, *v;
     float *ks, *vs;
     size_t layer_bytes, layer_scales;
-    u64 *counters;  // [0] page numbers that are none
-    u64 *host_pin;
+    u64 *counters;      // [0] page numbers that are none; behind it `arrived`
+    unsigned *arrived;  // [SISO_KV_WORKGROUPS], see kv_attend.hip; zeros between calls
     float *parts;  // what splits of a long axis leave for the one that joins them; see kv_attend.hip and kv_verify.hip
     size_t parts_floats;
     char err[256];

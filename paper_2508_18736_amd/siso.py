@@ -519,6 +519,7 @@ class PagedKV:
         self.kv_heads, self.head_dim, self.pages, self.page_tokens = int(kv_heads), int(head_dim), int(pages), int(page_tokens)
         self.layers, self.dtype, self.device = int(layers), int(dtype), torch.device(device)
         self._h = C.c_void_p()
+        self._index = torch.cuda.current_device() if self.device.index is None else self.device.index
         with torch.cuda.device(self.device):
             rc = _lib.siso_kv_create(self.layers, self.kv_heads, self.head_dim, self.page_tokens, self.pages, self.dtype,
                                      C.byref(self._h))
@@ -545,19 +546,19 @@ class PagedKV:
             pass
 
     def set_stream(self, stream: torch.cuda.Stream) -> None:
-        self._stream = stream
+        self._stream, self._raw_stream = stream, stream.cuda_stream
         self._check(_lib.siso_kv_set_stream(self._h, C.c_void_p(stream.cuda_stream)))
 
     def _used(self, *tensors: Optional[torch.Tensor]) -> None:
         """Memory that the handle's stream works on is not given to others before that work is done, where torch's
         allocator would count by another stream."""
-        if torch.cuda.current_stream(self.device) != self._stream:
+        if torch._C._cuda_getCurrentRawStream(self._index) != self._raw_stream:
             for t in tensors:
                 if t is not None:
                     t.record_stream(self._stream)
 
     def _heads(self, t: torch.Tensor, rows: int, heads: Optional[int], what: str) -> torch.Tensor:
-        if t.device != self.device or t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != rows or t.shape[2] != self.head_dim or \
+        if t.get_device() != self._index or t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != rows or t.shape[2] != self.head_dim or \
                 (heads is not None and t.shape[1] != heads):
             raise ValueError(f"{what}: expected a [{rows}, {'heads' if heads is None else heads}, {self.head_dim}] torch.bfloat16 "
                              f"tensor on {self.device}")
@@ -566,7 +567,7 @@ class PagedKV:
     def _out(self, t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str) -> torch.Tensor:
         if t is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
-        if t.device != self.device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        if t.get_device() != self._index or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{what}: expected a contiguous {list(shape)} {dtype} tensor on {self.device}")
         return t
 
@@ -576,7 +577,7 @@ class PagedKV:
         """Sequences for the calls below: rows ``first[b] .. first[b + 1] - 1`` (int32 [n + 1]) are the newest of the ``length[b]``
         tokens (int32 [n]) in the pages ``pages[b]`` (int32 [n, width]).  ``rows``: first[n] (None: asked of the GPU)."""
         for t, name, dims in ((first, "first", 1), (length, "length", 1), (pages, "pages", 2)):
-            if t is not None and (t.device != self.device or t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous()):
+            if t is not None and (t.get_device() != self._index or t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous()):
                 raise ValueError(f"{name}: expected a contiguous int32 tensor of {dims} dimension(s) on {self.device}")
         n = first.shape[0] - 1
         if n < 0 or (length is not None and length.shape[0] != n) or (pages is not None and pages.shape[0] != n) or \
@@ -627,12 +628,12 @@ class PagedKV:
         rows, n = batch.rows, batch.n
         for t, name, dtype, size in ((tokens, "tokens", torch.int32, rows), (u_accept, "u_accept", torch.float32, rows),
                                      (u_sample, "u_sample", torch.float32, n)):
-            if t is not None and (t.device != self.device or t.dtype != dtype or t.shape != (size,) or not t.is_contiguous()):
+            if t is not None and (t.get_device() != self._index or t.dtype != dtype or t.shape != (size,) or not t.is_contiguous()):
                 raise ValueError(f"{name}: expected a contiguous [{size}] {dtype} tensor on {self.device}")
         if target.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError("target: float32 or bfloat16")
         for t, name in ((target, "target"), (draft, "draft")):
-            if t is not None and (t.device != self.device or t.dtype != target.dtype or t.dim() != 2 or t.shape[0] != rows or
+            if t is not None and (t.get_device() != self._index or t.dtype != target.dtype or t.dim() != 2 or t.shape[0] != rows or
                                   t.shape[1] != target.shape[1] or t.stride(1) != 1):
                 raise ValueError(f"{name}: expected a [{rows}, vocab] {target.dtype} tensor on {self.device}, entries of a row side by side")
         out_accepted = self._out(out_accepted, (n,), torch.int32, "out_accepted")
