@@ -3,6 +3,7 @@
 #include <stdio.h>
 #include <string.h>
 #include <new>
+#include <type_traits>
 
 #include "kv_internal.h"
 
@@ -92,7 +93,7 @@ extern "C" int siso_kv_create(int layers, int kv_heads, int head_dim, int page_t
             ok = ok && hipMalloc((void **)&kv->ks, scales) == hipSuccess && hipMalloc((void **)&kv->vs, scales) == hipSuccess;
             ok = ok && hipMemset(kv->ks, 0, scales) == hipSuccess && hipMemset(kv->vs, 0, scales) == hipSuccess;
         }
-        const size_t counts = 32 * sizeof(u64) + SISO_KV_WORKGROUPS * sizeof(unsigned);
+        const size_t counts = 32 * sizeof(u64) + SISO_KV_JOINS * sizeof(unsigned);
         ok = ok && hipMalloc((void **)&kv->counters, counts) == hipSuccess;
         ok = ok && hipMemset(kv->counters, 0, counts) == hipSuccess;
         kv->arrived = (unsigned *)(kv->counters + 32);
@@ -177,6 +178,9 @@ __device__ __forceinline__ float kv_half_of(u32x4_t x, int i) {
 }
 
 // Eight elements of a vector that 16 threads hold (each 8 of NC * 128) as codes; the vector's scale.
+// Quotients are those of a correctly rounded division: y, 1 / scale rounded, is formed once for the vector, and two steps
+// q += (x - q scale) y, whose remainder is exact, end in the number closest to x / scale (Markstein).  Scales for which 1 / scale or a
+// remainder could leave the normal range take the division itself.
 template <int NC>
 __device__ __forceinline__ float kv_quantise(const u32x4_t (&x)[NC], uint2 (&codes)[NC]) {
     float amax = 0.f;
@@ -193,19 +197,76 @@ __device__ __forceinline__ float kv_quantise(const u32x4_t (&x)[NC], uint2 (&cod
     amax = wave_fold<8>(amax, [](float a, float b) __attribute__((always_inline)) { return fmaxf(a, b); });
     const bool bad = !(amax <= 3.4e38f);
     const float scale = amax / 448.0f;
-    const bool none = bad || scale == 0.f;
+    const bool none = bad || scale == 0.f, plain = !(scale > 1e-25f && scale < 1e25f);
+    const float y = __fdiv_rn(1.0f, scale);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        unsigned w[2] = {0, 0};
+        float q[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const unsigned code = none ? 0u : f32_to_e4m3(__fdiv_rn(kv_half_of(x[c], i), scale));
-            w[i >> 2] |= code << (8 * (i & 3));
+            const float v = kv_half_of(x[c], i);
+            q[i] = v * y;
+            q[i] = __fmaf_rn(__fmaf_rn(-q[i], scale, v), y, q[i]);
+            q[i] = __fmaf_rn(__fmaf_rn(-q[i], scale, v), y, q[i]);
         }
-        codes[c] = make_uint2(w[0], w[1]);
+        if (plain)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = none ? 0.f : __fdiv_rn(kv_half_of(x[c], i), scale);
+        // (nearest, ties to even; at most 448 and the rounding of the scale, which is 448)
+        int w0 = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), w1 = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], 0, false);
+        w0 = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w0, true);
+        w1 = __builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], w1, true);
+        codes[c] = make_uint2((unsigned)w0, (unsigned)w1);
     }
     return bad ? __uint_as_float(0x7FC00000u) : scale;
 }
+
+// Four dimensions of eight tokens change sides: in[token] = four elements side by side, out[dimension] = eight tokens side by side, and back.
+__device__ __forceinline__ void kv_turn(const unsigned (&in)[8], uint2 (&out)[4]) {  // of one byte
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const unsigned a = __builtin_amdgcn_perm(in[4 * half + 1], in[4 * half], 0x05010400u), b = __builtin_amdgcn_perm(in[4 * half + 1], in[4 * half], 0x07030602u);
+        const unsigned c = __builtin_amdgcn_perm(in[4 * half + 3], in[4 * half + 2], 0x05010400u), d = __builtin_amdgcn_perm(in[4 * half + 3], in[4 * half + 2], 0x07030602u);
+        const unsigned t[4] = {__builtin_amdgcn_perm(c, a, 0x05040100u), __builtin_amdgcn_perm(c, a, 0x07060302u), __builtin_amdgcn_perm(d, b, 0x05040100u),
+                               __builtin_amdgcn_perm(d, b, 0x07060302u)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) (half ? out[i].y : out[i].x) = t[i];
+    }
+}
+__device__ __forceinline__ void kv_turn_back(const uint2 (&in)[4], unsigned (&out)[8]) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        unsigned x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = half ? in[i].y : in[i].x;
+        const unsigned a = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), b = __builtin_amdgcn_perm(x[1], x[0], 0x07030602u);
+        const unsigned c = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u), d = __builtin_amdgcn_perm(x[3], x[2], 0x07030602u);
+        out[4 * half] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+        out[4 * half + 1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+        out[4 * half + 2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+        out[4 * half + 3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+    }
+}
+__device__ __forceinline__ void kv_turn(const uint2 (&in)[8], u32x4_t (&out)[4]) {  // of two bytes
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // two tokens
+        out[0][i] = __builtin_amdgcn_perm(in[2 * i + 1].x, in[2 * i].x, 0x05040100u);
+        out[1][i] = __builtin_amdgcn_perm(in[2 * i + 1].x, in[2 * i].x, 0x07060302u);
+        out[2][i] = __builtin_amdgcn_perm(in[2 * i + 1].y, in[2 * i].y, 0x05040100u);
+        out[3][i] = __builtin_amdgcn_perm(in[2 * i + 1].y, in[2 * i].y, 0x07060302u);
+    }
+}
+__device__ __forceinline__ void kv_turn_back(const u32x4_t (&in)[4], uint2 (&out)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        out[2 * i].x = __builtin_amdgcn_perm(in[1][i], in[0][i], 0x05040100u);
+        out[2 * i + 1].x = __builtin_amdgcn_perm(in[1][i], in[0][i], 0x07060302u);
+        out[2 * i].y = __builtin_amdgcn_perm(in[3][i], in[2][i], 0x05040100u);
+        out[2 * i + 1].y = __builtin_amdgcn_perm(in[3][i], in[2][i], 0x07060302u);
+    }
+}
+__device__ __forceinline__ int kv_token(int half, int s) { return (s & 3) + 4 * half + 8 * (s >> 2); }  // of a half's eight
+__device__ __forceinline__ size_t kv_v8_at(int dp, int h, int d) { return (((h * (dp >> 6) + (d >> 6)) * 32 + (d & 31)) * 2 + ((d >> 5) & 1)) * 8; }
 
 // NC: chunks of 8 elements per thread (dp <= 128: one, else two)
 template <int NC, bool FP8>
@@ -254,39 +315,41 @@ __global__ __launch_bounds__(256) void k_kv_write(KvPool pool, KvBatch batch, co
         }
     }
     __syncthreads();
-    // which tokens of the block are new: bit `key`
+    // which tokens of the block are new
     const int lo = blk.s.start > blk.at ? blk.s.start - blk.at : 0, hi = blk.s.length - blk.at < 16 ? blk.s.length - blk.at : 16;
-    for (int j = t; j < 2 * dp; j += 256) {
-        const int h = j >= dp, d = j - h * dp;
-        if (d >= dim) continue;
+    for (int j = t; j < dp >> 1; j += 256) {  // a half's eight tokens, four dimensions
+        const int h = j >= dp >> 2, d0 = 4 * (j - h * (dp >> 2));
+        if (d0 >= dim) continue;
         if constexpr (FP8) {
-            char *to = vb + (((h * (dp >> 6) + (d >> 6)) * 32 + (d & 31)) * 2 + ((d >> 5) & 1)) * 8;
-            unsigned w[2] = {0, 0};
+            unsigned x[8];
+            uint2 y[4];
 #pragma unroll
-            for (int s = 0; s < 8; ++s) w[s >> 2] |= (unsigned)(unsigned char)turn[((s & 3) + 4 * h + 8 * (s >> 2)) * (DP + 8) + d] << (8 * (s & 3));
-            if (lo == 0 && hi == 16) *(uint2 *)to = make_uint2(w[0], w[1]);
-            else
+            for (int s = 0; s < 8; ++s) x[s] = *(const unsigned *)(turn + kv_token(h, s) * (DP + 8) + d0);
+            kv_turn(x, y);
 #pragma unroll
-                for (int s = 0; s < 8; ++s) {
-                    const int token = (s & 3) + 4 * h + 8 * (s >> 2);
-                    if (token >= lo && token < hi) to[s] = (char)(w[s >> 2] >> (8 * (s & 3)));
-                }
+            for (int c = 0; c < 4; ++c) {
+                char *to = vb + kv_v8_at(dp, h, d0 + c);
+                if (lo == 0 && hi == 16) *(uint2 *)to = y[c];
+                else
+#pragma unroll
+                    for (int s = 0; s < 8; ++s)
+                        if (kv_token(h, s) >= lo && kv_token(h, s) < hi) to[s] = (char)((s < 4 ? y[c].x : y[c].y) >> (8 * (s & 3)));
+            }
         } else {
-            bf16_t *to = (bf16_t *)vb + (h * dp + d) * 8;
-            bf16_t w[8];
+            uint2 x[8];
+            u32x4_t y[4];
 #pragma unroll
-            for (int s = 0; s < 8; ++s) w[s] = ((const bf16_t *)turn)[((s & 3) + 4 * h + 8 * (s >> 2)) * (DP + 8) + d];
-            if (lo == 0 && hi == 16) {
-                u32x4_t x;
+            for (int s = 0; s < 8; ++s) x[s] = *(const uint2 *)(turn + (kv_token(h, s) * (DP + 8) + d0) * 2);
+            kv_turn(x, y);
 #pragma unroll
-                for (int s = 0; s < 4; ++s) x[s] = (unsigned)w[2 * s] | ((unsigned)w[2 * s + 1] << 16);
-                *(u32x4_t *)to = x;
-            } else
+            for (int c = 0; c < 4; ++c) {
+                bf16_t *to = (bf16_t *)vb + (h * dp + d0 + c) * 8;
+                if (lo == 0 && hi == 16) *(u32x4_t *)to = y[c];
+                else
 #pragma unroll
-                for (int s = 0; s < 8; ++s) {
-                    const int token = (s & 3) + 4 * h + 8 * (s >> 2);
-                    if (token >= lo && token < hi) to[s] = w[s];
-                }
+                    for (int s = 0; s < 8; ++s)
+                        if (kv_token(h, s) >= lo && kv_token(h, s) < hi) to[s] = (bf16_t)(s & 1 ? y[c][s >> 1] >> 16 : y[c][s >> 1]);
+            }
         }
     }
 }
@@ -297,15 +360,20 @@ __device__ __forceinline__ void kv_store8(O *to, const float (&x)[8]) {
         *(float4 *)to = make_float4(x[0], x[1], x[2], x[3]);
         *(float4 *)(to + 4) = make_float4(x[4], x[5], x[6], x[7]);
     } else {
-        u32x4_t w;
+        struct {
+            __bf16 v[8];
+        } w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (unsigned)f32_to_bf16(x[2 * i]) | ((unsigned)f32_to_bf16(x[2 * i + 1]) << 16);
-        *(u32x4_t *)to = w;
+        for (int i = 0; i < 8; ++i) w.v[i] = (__bf16)x[i];
+        *(u32x4_t *)to = __builtin_bit_cast(u32x4_t, w);
     }
 }
 __device__ __forceinline__ void kv_decode8(uint2 codes, float scale, float (&x)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = e4m3_to_f32(((i < 4 ? codes.x : codes.y) >> (8 * (i & 3))) & 255u) * scale;
+    for (int i = 0; i < 2; ++i) {
+        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)(i ? codes.y : codes.x), false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)(i ? codes.y : codes.x), true);
+        x[4 * i] = a[0] * scale, x[4 * i + 1] = a[1] * scale, x[4 * i + 2] = b[0] * scale, x[4 * i + 3] = b[1] * scale;
+    }
 }
 
 template <int NC, bool FP8, class O>
@@ -339,44 +407,48 @@ __global__ __launch_bounds__(256) void k_kv_read(KvPool pool, KvBatch batch, O *
     const bool in = row >= 0 && row < blk.s.rows;
     const bool held = blk.page >= 0;
     const int page = held ? blk.page : 0;
+    using K = typename std::conditional<FP8, uint2, u32x4_t>::type;       // eight elements
+    using Four = typename std::conditional<FP8, unsigned, uint2>::type;  // four
+    const int vh = t >= dp >> 2, vd = 4 * (t - vh * (dp >> 2));             // the half and the four dimensions that this thread turns
+    K kx[NC], vx[4];
+    float ksc = 1.f, vsc = 1.f;
     const char *kb = pool.k + kv_block_at(pool, page, head, blk.at) * ES;
     const char *vb = pool.v + kv_block_at(pool, page, head, blk.at) * ES;
-    for (int j = t; j < 2 * dp; j += 256) {
-        const int h = j >= dp, d = j - h * dp;
-        if constexpr (FP8) {
-            const uint2 w = *(const uint2 *)(vb + (((h * (dp >> 6) + (d >> 6)) * 32 + (d & 31)) * 2 + ((d >> 5) & 1)) * 8);
 #pragma unroll
-            for (int s = 0; s < 8; ++s)
-                turn[((s & 3) + 4 * h + 8 * (s >> 2)) * (DP + 8) + d] = (char)((s < 4 ? w.x : w.y) >> (8 * (s & 3)));
-        } else {
-            const u32x4_t w = *(const u32x4_t *)(vb + (size_t)(h * dp + d) * 16);
-#pragma unroll
-            for (int s = 0; s < 8; ++s)
-                ((bf16_t *)turn)[((s & 3) + 4 * h + 8 * (s >> 2)) * (DP + 8) + d] = (bf16_t)(s & 1 ? w[s >> 1] >> 16 : w[s >> 1]);
-        }
+    for (int c = 0; c < NC; ++c) {
+        const int e8 = i + 16 * c;
+        if (e8 * 8 < dp) kx[c] = *(const K *)(FP8 ? kb + ((e8 >> 1) * 16 + key) * 16 + (e8 & 1) * 8 : kb + (e8 * 16 + key) * 16);
     }
-    float ksc = 1.f, vsc = 1.f;
+    if (t < dp >> 1)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) vx[c] = *(const K *)(FP8 ? vb + kv_v8_at(dp, vh, vd + c) : vb + (size_t)(vh * dp + vd + c) * 16);
     if constexpr (FP8) {
         const size_t at = kv_scale_at(pool, page, head, blk.at) + key;
         ksc = pool.ks[at];
         vsc = pool.vs[at];
     }
+    if (t < dp >> 1) {
+        Four x[8];
+        kv_turn_back(vx, x);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) *(Four *)(turn + (kv_token(vh, s) * (DP + 8) + vd) * ES) = x[s];
+    }
     __syncthreads();
     if (!in) return;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int e8 = i + 16 * c, e = 8 * e8;
+        const int e = 8 * (i + 16 * c);
         if (e >= dim) continue;
         float x[8], y[8];
+        const K vv = *(const K *)(turn + (key * (DP + 8) + e) * ES);
         if constexpr (FP8) {
-            kv_decode8(*(const uint2 *)(kb + ((e8 >> 1) * 16 + key) * 16 + (e8 & 1) * 8), ksc, x);
-            kv_decode8(*(const uint2 *)(turn + key * (DP + 8) + e), vsc, y);
+            kv_decode8(kx[c], ksc, x);
+            kv_decode8(vv, vsc, y);
         } else {
-            const u32x4_t a = *(const u32x4_t *)(kb + (e8 * 16 + key) * 16), b = *(const u32x4_t *)(turn + (key * (DP + 8) + e) * 2);
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
-                x[s] = kv_half_of(a, s);
-                y[s] = kv_half_of(b, s);
+                x[s] = kv_half_of(kx[c], s);
+                y[s] = kv_half_of(vv, s);
             }
         }
         if (!held)

@@ -93,7 +93,7 @@ __device__ __forceinline__ size_t kv_scale_at(const KvPool &pool, int page, int 
 }
 #endif
 
-#define SISO_KV_WORKGROUPS 512  // of a launch that leaves parts to be joined, at most
+#define SISO_KV_JOINS 65536  // sequences of a batch; workgroups of an attention launch that leaves parts to be joined are fewer
 
 struct siso_kv {
     int layers, kv_heads, dim, dp, page_tokens, dtype;
@@ -103,7 +103,7 @@ struct siso_kv {
     float *ks, *vs;
     size_t layer_bytes, layer_scales;
     u64 *counters;      // [0] page numbers that are none; behind it `arrived`
-    unsigned *arrived;  // [SISO_KV_WORKGROUPS], see kv_attend.hip; zeros between calls
+    unsigned *arrived;  // [SISO_KV_JOINS] how many parts are there of what several workgroups work on; zeros between calls
     float *parts;  // what splits of a long axis leave for the one that joins them; see kv_attend.hip and kv_verify.hip
     size_t parts_floats;
     char err[256];

@@ -10,10 +10,13 @@ struct KvVerify {
     const float *u_accept, *u_sample;
     int *accepted, *out;
     int slices, slice;  // the vocabulary in slices of `slice` entries, a multiple of KV_SLICE_UNIT
-    double *sums;       // [n][slices] sums of the weights
-    u64 *best;          // greedy: [rows][slices] largest entry and its place, as keys
+    u64 *parts;         // [n][slices] sums of the weights, as their bits; greedy: [rows][slices] largest entry and its place, as keys
+    unsigned *arrived;  // [n] slices of a sequence that are done; zeros between calls
+    int lanes;          // greedy: workgroups that share a sequence's rows
     long item0;
 };
+#define KV_SLICES 256  // of a row, at most: one for each thread of the workgroup that joins them
+#define KV_FILL 2048 // workgroups
 #define KV_SLICE_UNIT 2048  // 256 threads, eight entries each
 
 // Eight entries from e on of a row that begins anywhere (a row of an odd vocabulary is aligned to its type only).
@@ -96,26 +99,20 @@ __device__ __forceinline__ double kv_wave_sum(double v) {
     return wave_fold(v, [](double a, double b) __attribute__((always_inline)) { return a + b; });
 }
 
-// One slice of one sequence's row: the sum of its weights.
-template <class T>
-__global__ __launch_bounds__(256) void k_kv_sums(KvVerify a) {
-    __shared__ double part[4];
-    const int b = (int)(blockIdx.x / a.slices), slice = blockIdx.x % a.slices;
-    const KvSequence s = kv_sequence(a.batch, b);
-    if (s.rows == 0) return;
-    const KvWeights<T> weights = kv_weights<T>(a, s, kv_accepted<T>(a, s));
-    double sum = 0.0;
-    const int end = (slice + 1) * a.slice < a.vocab ? (slice + 1) * a.slice : a.vocab;
-    for (int e = slice * a.slice + 8 * threadIdx.x; e < end; e += KV_SLICE_UNIT) {
-        double w[8];
-        weights.eight(e, a.vocab, w);
-        sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+// Numbers of a workgroup for the one that is done last with a sequence.  They pass the caches of the XCDs (see kv_attend.hip).  All that
+// decides how many workgroups come is the same for all of them, whatever the batch's numbers are: the count is always reached.
+__device__ __forceinline__ void kv_leave_part(u64 *to, u64 what) { __hip_atomic_store(to, what, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ bool kv_last(unsigned *arrived, unsigned count) {  // thread 0 has left all numbers; true in the workgroup that is last
+    __shared__ int last;
+    if (threadIdx.x == 0) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // they are where all workgroups see them
+        last = atomicAdd(arrived, 1u) == count - 1;
+        if (last) *arrived = 0;  // (for the next call: nobody else comes)
     }
-    sum = kv_wave_sum(sum);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) a.sums[(long)b * a.slices + slice] = (part[0] + part[1]) + (part[2] + part[3]);
+    return last;
 }
+__device__ __forceinline__ u64 kv_part(const u64 *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // The first entry of [begin, end) at which the running sum, `before` behind the entries ahead, exceeds `bar`; the last entry with
 // weight where rounding leaves none; -1 where nothing has weight.  All 256 threads.  total: the sum of all.
@@ -178,34 +175,74 @@ __device__ __forceinline__ void kv_write_tokens(const KvVerify &a, const KvSeque
     if (threadIdx.x == 0) a.accepted[s.b] = accepted;
 }
 
+// Running sums over the 256 threads of a workgroup; `all`: the sum of all.
+__device__ __forceinline__ double kv_running_sum(double v, double *all) {
+    __shared__ double waves[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const double x = __shfl_up(v, off);
+        if (lane >= off) v += x;
+    }
+    if (lane == 63) waves[wave] = v;
+    __syncthreads();
+    double before = 0.0;
+    for (int i = 0; i < wave; ++i) before += waves[i];
+    *all = ((waves[0] + waves[1]) + waves[2]) + waves[3];
+    __syncthreads();
+    return before + v;
+}
+
+// One slice of one sequence's row: the sum of its weights.  The workgroup that is done last with a sequence draws its token.
 template <class T>
-__global__ __launch_bounds__(256) void k_kv_choose(KvVerify a) {
-    const int b = blockIdx.x;
+__global__ __launch_bounds__(256) void k_kv_draw(KvVerify a) {
+    __shared__ double part[4], upto[KV_SLICES];
+    __shared__ int found[4], has[4];
+    const int b = (int)((a.item0 + blockIdx.x) / a.slices), slice = (int)((a.item0 + blockIdx.x) % a.slices), t = threadIdx.x;
     const KvSequence s = kv_sequence(a.batch, b);
     if (s.rows == 0) {
-        if (threadIdx.x == 0) a.accepted[b] = -1;
+        if (slice == 0 && t == 0) a.accepted[b] = -1;
         return;
     }
     const int accepted = kv_accepted<T>(a, s);
     KvWeights<T> weights = kv_weights<T>(a, s, accepted);
-    const double *sums = a.sums + (long)b * a.slices;
-    double total = 0.0;
-    for (int i = 0; i < a.slices; ++i) total += sums[i];
+    double sum = 0.0;
+    const int end = (slice + 1) * a.slice < a.vocab ? (slice + 1) * a.slice : a.vocab;
+    for (int e = slice * a.slice + 8 * t; e < end; e += KV_SLICE_UNIT) {
+        double w[8];
+        weights.eight(e, a.vocab, w);
+        sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    }
+    sum = kv_wave_sum(sum);
+    if ((t & 63) == 0) part[t >> 6] = sum;
+    __syncthreads();
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
+    u64 *parts = a.parts + (long)b * a.slices;
+    if (t == 0) kv_leave_part(parts + slice, (u64)__double_as_longlong(sum));
+    if (!kv_last(a.arrived + b, a.slices)) return;
+
+    const double mine = t < a.slices ? __longlong_as_double((long long)kv_part(parts + t)) : 0.0;
+    double total;
+    const double run = kv_running_sum(mine, &total);
     const double u = (double)fminf(fmaxf(a.u_sample[b], 0.f), 0.99999994f);
     int following;
     double ignored;
     if (total > 0.0) {
+        // the first slice with weight in which the bar is passed, or the last one with weight
         const double bar = u * total;
-        double before = 0.0;
-        int slice = -1;
-        for (int i = 0; i < a.slices; ++i) {  // the slice in which the bar is passed, or the last one with weight
-            if (!(sums[i] > 0.0)) continue;
-            if (slice >= 0) before += sums[slice];
-            slice = i;
-            if (before + sums[i] > bar) break;
+        if (t < KV_SLICES) upto[t] = run;
+        const u64 over = __ballot(mine > 0.0 && run > bar), some = __ballot(mine > 0.0);
+        if ((t & 63) == 0) {
+            found[t >> 6] = over ? (t & ~63) + __ffsll((long long)over) - 1 : -1;
+            has[t >> 6] = some ? (t & ~63) + 63 - __clzll((long long)some) : -1;
         }
-        const int begin = slice * a.slice;
-        following = kv_find(weights, begin, begin + a.slice < a.vocab ? begin + a.slice : a.vocab, a.vocab, before, bar, &ignored);
+        __syncthreads();
+        int at = -1;
+        for (int i = 3; i >= 0; --i) at = found[i] >= 0 ? found[i] : at;
+        if (at < 0)
+            for (int i = 0; i < 4; ++i) at = has[i] >= 0 ? has[i] : at;
+        const int begin = at * a.slice;
+        following = kv_find(weights, begin, begin + a.slice < a.vocab ? begin + a.slice : a.vocab, a.vocab, at > 0 ? upto[at - 1] : 0.0, bar, &ignored);
     } else {  // the target's own probabilities, if there are any
         weights.q = nullptr;
         weights.not_this = -1;
@@ -215,65 +252,91 @@ __global__ __launch_bounds__(256) void k_kv_choose(KvVerify a) {
     kv_write_tokens(a, s, accepted, following);
 }
 
-// Greedy: one slice of one row, its largest entry as a key that orders equal entries by their place.
+// Greedy: one slice of every a.lanes-th row of a sequence, the largest entries as keys that order equal ones by their place, four rows
+// at a time.  The workgroup that is done last with a sequence compares the draft with them.
 template <class T>
-__global__ __launch_bounds__(256) void k_kv_largest(KvVerify a) {
-    __shared__ u64 part[4];
-    const long item = a.item0 + blockIdx.x, row = item / a.slices;
-    const int slice = (int)(item % a.slices);
-    const T *x = (const T *)a.target + row * a.target_stride;
-    const int end = (slice + 1) * a.slice < a.vocab ? (slice + 1) * a.slice : a.vocab;
-    float top = -INFINITY;
-    int at = -1;
-    for (int e = slice * a.slice + 8 * threadIdx.x; e < end; e += KV_SLICE_UNIT) {
-        float v[8];
-        if (e + 8 <= a.vocab) kv_entries8(x + e, v);
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = e + i < a.vocab ? widen(x[e + i]) : __uint_as_float(0x7FC00000u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (v[i] > top || (at < 0 && v[i] == top)) {
-                top = v[i];
-                at = e + i;
-            }
-    }
-    u64 key = at < 0 ? 0 : pack_key(top + 0.f, (unsigned)at);  // (+ 0: the two zeros are equal)
-    key = wave_max(key);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = key;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 4; ++i) key = part[i] > key ? part[i] : key;
-        a.best[row * a.slices + slice] = key;
-    }
-}
-
-__global__ __launch_bounds__(64) void k_kv_follow_largest(KvVerify a) {
-    const int b = blockIdx.x, lane = threadIdx.x;
+__global__ __launch_bounds__(256) void k_kv_follow(KvVerify a) {
+    constexpr int ROWS = 4;
+    __shared__ u64 part[ROWS][4];
+    const long item = a.item0 + blockIdx.x;
+    const int slice = (int)(item % a.slices), lead = (int)(item / a.slices % a.lanes), b = (int)(item / a.slices / a.lanes), t = threadIdx.x;
     const KvSequence s = kv_sequence(a.batch, b);
     if (s.rows == 0) {
-        if (lane == 0) a.accepted[b] = -1;
+        if (slice == 0 && lead == 0 && t == 0) a.accepted[b] = -1;
         return;
     }
+    if (lead >= s.rows) return;
+    const int end = (slice + 1) * a.slice < a.vocab ? (slice + 1) * a.slice : a.vocab;
+    for (int i0 = lead; i0 < s.rows; i0 += ROWS * a.lanes) {
+        float top[ROWS];
+        int at[ROWS];
+        const T *x[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            top[r] = -INFINITY;
+            at[r] = -1;
+            x[r] = (const T *)a.target + (long)(s.first + (i0 + r * a.lanes < s.rows ? i0 + r * a.lanes : i0)) * a.target_stride;
+        }
+        for (int e = slice * a.slice + 8 * t; e < end; e += KV_SLICE_UNIT) {
+            float v[ROWS][8];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                if (r > 0 && i0 + r * a.lanes >= s.rows) break;
+                if (e + 8 <= a.vocab) kv_entries8(x[r] + e, v[r]);
+                else
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[r][i] = e + i < a.vocab ? widen(x[r][e + i]) : __uint_as_float(0x7FC00000u);
+            }
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                if (r > 0 && i0 + r * a.lanes >= s.rows) break;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (v[r][i] > top[r] || (at[r] < 0 && v[r][i] == top[r])) {
+                        top[r] = v[r][i];
+                        at[r] = e + i;
+                    }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const u64 key = wave_max(at[r] < 0 ? (u64)0 : pack_key(top[r] + 0.f, (unsigned)at[r]));  // (+ 0: the two zeros are equal)
+            if ((t & 63) == 0) part[r][t >> 6] = key;
+        }
+        __syncthreads();
+        if (t == 0)
+            for (int r = 0; r < ROWS && i0 + r * a.lanes < s.rows; ++r) {
+                u64 key = part[r][0];
+                for (int i = 1; i < 4; ++i) key = part[r][i] > key ? part[r][i] : key;
+                kv_leave_part(a.parts + (long)(s.first + i0 + r * a.lanes) * a.slices + slice, key);
+            }
+        __syncthreads();
+    }
+    if (!kv_last(a.arrived + b, (unsigned)(s.rows < a.lanes ? s.rows : a.lanes) * a.slices)) return;
+
     int accepted = 0, following = -1;
-    for (int i0 = 0; i0 < s.rows; i0 += 64) {
-        const int i = i0 + lane;
+    for (int i0 = 0; i0 < s.rows; i0 += 64) {  // (every wave by itself)
+        const int i = i0 + (t & 63);
         int best = -1;
         bool good = false;
         if (i < s.rows) {
-            u64 key = 0;
-            for (int j = 0; j < a.slices; ++j) {
-                const u64 k = a.best[(long)(s.first + i) * a.slices + j];
-                key = k > key ? k : key;
+            u64 most = 0;
+            const u64 *of_row = a.parts + (long)(s.first + i) * a.slices;
+            for (int j = 0; j < a.slices; j += 8) {
+                u64 k[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) k[c] = kv_part(of_row + (j + c < a.slices ? j + c : j));
+#pragma unroll
+                for (int c = 0; c < 8; ++c) most = k[c] > most ? k[c] : most;
             }
-            if (key != 0) best = (int)(0xFFFFFFFFu - (unsigned)key);
+            if (most != 0) best = (int)(0xFFFFFFFFu - (unsigned)most);
             good = i < s.rows - 1 && best >= 0 && best == a.tokens[s.first + i + 1];
         }
         const u64 refused = ~__ballot(good);
-        const int at = refused ? __ffsll((long long)refused) - 1 : 64;
-        accepted = i0 + at;
-        following = __shfl(best, at & 63);
-        if (at < 64) break;  // (the last row is never `good`: this ends at the latest there)
+        const int stop = refused ? __ffsll((long long)refused) - 1 : 64;
+        accepted = i0 + stop;
+        following = __shfl(best, stop & 63);
+        if (stop < 64) break;  // (the last row is never `good`: this ends at the latest there)
     }
     kv_write_tokens(a, s, accepted, following);
 }
@@ -304,35 +367,31 @@ extern "C" int siso_kv_verify(siso_kv *kv, const siso_kv_batch *batch, const int
     a.u_sample = u_sample;
     a.accepted = out_accepted;
     a.out = out_tokens;
-    a.sums = (double *)kv->parts;
-    a.best = (u64 *)kv->parts;
+    a.parts = (u64 *)kv->parts;
+    a.arrived = kv->arrived;
     a.item0 = 0;
-    // as many slices as fill the chip (2,048 workgroups), of one unit at least; one key or sum each fits the workspace: at most 2,048 or the items
-    const long items = u_accept ? a.batch.n : a.batch.rows > 0 ? a.batch.rows : 1;
-    const long units = (vocab + KV_SLICE_UNIT - 1) / KV_SLICE_UNIT;
-    long slices = 2048 / items;
+    // as many slices as fill the chip, of one unit at least (a part of each fits the workspace: KV_FILL of them, or one for each row)
+    const long units = (vocab + KV_SLICE_UNIT - 1) / KV_SLICE_UNIT, rows = a.batch.rows > 0 ? a.batch.rows : 1;
+    const long max_new = batch->max_new > 0 && batch->max_new < rows ? batch->max_new : rows;
+    long slices = KV_FILL / (u_accept ? a.batch.n : rows);
+    slices = slices > KV_SLICES ? KV_SLICES : slices;
     slices = slices < 1 ? 1 : slices > units ? units : slices;
     a.slice = (int)((units + slices - 1) / slices * KV_SLICE_UNIT);
     a.slices = (vocab + a.slice - 1) / a.slice;
-    const long all = items * a.slices, piece = 1L << 23;
-    if (u_accept) {
-        const dim3 grid((unsigned)all);
-        if (type == SISO_F32) {
-            hipLaunchKernelGGL(k_kv_sums<float>, grid, dim3(256), 0, kv->stream, a);
-            hipLaunchKernelGGL(k_kv_choose<float>, dim3((unsigned)a.batch.n), dim3(256), 0, kv->stream, a);
-        } else {
-            hipLaunchKernelGGL(k_kv_sums<bf16_t>, grid, dim3(256), 0, kv->stream, a);
-            hipLaunchKernelGGL(k_kv_choose<bf16_t>, dim3((unsigned)a.batch.n), dim3(256), 0, kv->stream, a);
-        }
-    } else {
-        for (a.item0 = 0; a.item0 < all && a.batch.rows > 0; a.item0 += piece) {
-            const dim3 grid((unsigned)(all - a.item0 < piece ? all - a.item0 : piece));
-            if (type == SISO_F32) hipLaunchKernelGGL(k_kv_largest<float>, grid, dim3(256), 0, kv->stream, a);
-            else hipLaunchKernelGGL(k_kv_largest<bf16_t>, grid, dim3(256), 0, kv->stream, a);
-            KV_TRY(kv, hipGetLastError());
-        }
-        hipLaunchKernelGGL(k_kv_follow_largest, dim3((unsigned)a.batch.n), dim3(64), 0, kv->stream, a);
+    a.lanes = 1;
+    if (!u_accept) {  // four rows keep a workgroup busy
+        long lanes = KV_FILL / ((long)a.batch.n * a.slices);
+        lanes = lanes > (max_new + 3) / 4 ? (max_new + 3) / 4 : lanes;
+        a.lanes = lanes < 1 ? 1 : (int)lanes;
     }
-    KV_TRY(kv, hipGetLastError());
+    const long all = (long)a.batch.n * a.slices * a.lanes, piece = 1L << 23;
+    for (; a.item0 < all; a.item0 += piece) {  // (a launch has fewer than 2^32 threads)
+        const dim3 grid((unsigned)(all - a.item0 < piece ? all - a.item0 : piece));
+        if (u_accept && type == SISO_F32) hipLaunchKernelGGL(k_kv_draw<float>, grid, dim3(256), 0, kv->stream, a);
+        else if (u_accept) hipLaunchKernelGGL(k_kv_draw<bf16_t>, grid, dim3(256), 0, kv->stream, a);
+        else if (type == SISO_F32) hipLaunchKernelGGL(k_kv_follow<float>, grid, dim3(256), 0, kv->stream, a);
+        else hipLaunchKernelGGL(k_kv_follow<bf16_t>, grid, dim3(256), 0, kv->stream, a);
+        KV_TRY(kv, hipGetLastError());
+    }
     return SISO_OK;
 }

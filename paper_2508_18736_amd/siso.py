@@ -549,20 +549,27 @@ class PagedKV:
         self._stream, self._raw_stream = stream, stream.cuda_stream
         self._check(_lib.siso_kv_set_stream(self._h, C.c_void_p(stream.cuda_stream)))
 
+    def _elsewhere(self) -> bool:
+        """Does the handle's stream differ from torch's current one?"""
+        return torch._C._cuda_getCurrentRawStream(self._index) != self._raw_stream
+
     def _used(self, *tensors: Optional[torch.Tensor]) -> None:
         """Memory that the handle's stream works on is not given to others before that work is done, where torch's
         allocator would count by another stream."""
-        if torch._C._cuda_getCurrentRawStream(self._index) != self._raw_stream:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self._stream)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self._stream)
 
     def _heads(self, t: torch.Tensor, rows: int, heads: Optional[int], what: str) -> torch.Tensor:
-        if t.get_device() != self._index or t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] != rows or t.shape[2] != self.head_dim or \
-                (heads is not None and t.shape[1] != heads):
+        shape = t.shape
+        if t.get_device() != self._index or t.dtype != torch.bfloat16 or len(shape) != 3 or shape[0] != rows or shape[2] != self.head_dim or \
+                (heads is not None and shape[1] != heads):
             raise ValueError(f"{what}: expected a [{rows}, {'heads' if heads is None else heads}, {self.head_dim}] torch.bfloat16 "
                              f"tensor on {self.device}")
-        return t if t.stride(2) == 1 else t.contiguous()
+        if t.stride(2) == 1:
+            return t
+        with torch.cuda.stream(self._stream):  # (a copy is ordered like the call)
+            return t.contiguous()
 
     def _out(self, t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str) -> torch.Tensor:
         if t is None:
@@ -588,7 +595,8 @@ class PagedKV:
     def write(self, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, layer: int = 0) -> None:
         k = self._heads(k, batch.rows, self.kv_heads, "k")
         v = self._heads(v, batch.rows, self.kv_heads, "v")
-        self._used(k, v, *batch.tensors)
+        if self._elsewhere():
+            self._used(k, v, *batch.tensors)
         self._check(_lib.siso_kv_write(self._h, layer, batch._ref, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
                                        v.stride(1)))
 
@@ -599,7 +607,8 @@ class PagedKV:
             raise ValueError("dtype: torch.bfloat16 or torch.float32")
         shape = (batch.rows, self.kv_heads, self.head_dim)
         out_k, out_v = self._out(out_k, shape, dtype, "out_k"), self._out(out_v, shape, dtype, "out_v")
-        self._used(out_k, out_v, *batch.tensors)
+        if self._elsewhere():
+            self._used(out_k, out_v, *batch.tensors)
         self._check(_lib.siso_kv_read(self._h, layer, batch._ref, F32 if dtype == torch.float32 else BF16, out_k.data_ptr(),
                                       out_v.data_ptr()))
         return out_k, out_v
@@ -609,14 +618,17 @@ class PagedKV:
         """Attention of ``q`` [rows, heads, head_dim] (scale: 1 / sqrt(head_dim) unless given): ``out``, or ``(out, lse)`` if ``lse``
         is given or asked for."""
         q = self._heads(q, batch.rows, None, "q")
-        shape = tuple(q.shape)
-        out = self._out(out, shape, torch.bfloat16, "out")
+        shape, stride = q.shape, q.stride()
+        out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else self._out(out, shape, torch.bfloat16, "out")
         if with_lse or lse is not None:
             lse = self._out(lse, shape[:2], torch.float32, "lse")
-        self._used(q, out, lse, *batch.tensors)
-        self._check(_lib.siso_kv_attend(self._h, layer, batch._ref, q.data_ptr(), q.stride(0), q.stride(1), shape[1],
-                                        self.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
-                                        None if lse is None else lse.data_ptr()))
+        if self._elsewhere():
+            self._used(q, out, lse, *batch.tensors)
+        rc = _lib.siso_kv_attend(self._h, layer, batch._ref, q.data_ptr(), stride[0], stride[1], shape[1],
+                                 self.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
+                                 None if lse is None else lse.data_ptr())
+        if rc < 0:
+            self._check(rc)
         return out if lse is None else (out, lse)
 
     def verify(self, batch: KvBatch, tokens: torch.Tensor, target: torch.Tensor, draft: Optional[torch.Tensor] = None,
@@ -637,8 +649,9 @@ class PagedKV:
                                   t.shape[1] != target.shape[1] or t.stride(1) != 1):
                 raise ValueError(f"{name}: expected a [{rows}, vocab] {target.dtype} tensor on {self.device}, entries of a row side by side")
         out_accepted = self._out(out_accepted, (n,), torch.int32, "out_accepted")
-        out_tokens = self._out(out_tokens, (rows,), torch.int32, "out_tokens")
-        self._used(tokens, target, draft, u_accept, u_sample, out_accepted, out_tokens, *batch.tensors)
+        out_tokens = torch.empty_like(tokens) if out_tokens is None else self._out(out_tokens, (rows,), torch.int32, "out_tokens")
+        if self._elsewhere():
+            self._used(tokens, target, draft, u_accept, u_sample, out_accepted, out_tokens, *batch.tensors)
         p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         self._check(_lib.siso_kv_verify(self._h, batch._ref, tokens.data_ptr(), target.shape[1], F32 if target.dtype == torch.float32 else BF16,
                                         target.data_ptr(), target.stride(0), p(draft), 0 if draft is None else draft.stride(0),
