@@ -78,7 +78,6 @@ extern "C" int siso_kv_create(int layers, int kv_heads, int head_dim, int page_t
     kv->page_tokens = page_tokens;
     kv->pages = pages;
     kv->dtype = dtype;
-    kv->parts_floats = (size_t)32 << 20;  // 128 MiB: the splits of a call are chosen to stay within it
     // (sizes of 2^63 and more would wrap: no GPU has as much)
     const double all = (double)layers * pages * page_tokens * kv_heads * kv->dp * 2;
     bool ok = all < 1e15;
@@ -93,11 +92,12 @@ extern "C" int siso_kv_create(int layers, int kv_heads, int head_dim, int page_t
             ok = ok && hipMalloc((void **)&kv->ks, scales) == hipSuccess && hipMalloc((void **)&kv->vs, scales) == hipSuccess;
             ok = ok && hipMemset(kv->ks, 0, scales) == hipSuccess && hipMemset(kv->vs, 0, scales) == hipSuccess;
         }
-        const size_t counts = 32 * sizeof(u64) + SISO_KV_JOINS * sizeof(unsigned);
+        const size_t counts = 32 * sizeof(u64) + SISO_KV_JOINS * sizeof(unsigned) + SISO_KV_PLAN_BYTES;
         ok = ok && hipMalloc((void **)&kv->counters, counts) == hipSuccess;
         ok = ok && hipMemset(kv->counters, 0, counts) == hipSuccess;
         kv->arrived = (unsigned *)(kv->counters + 32);
-        ok = ok && hipMalloc((void **)&kv->parts, kv->parts_floats * sizeof(float)) == hipSuccess;
+        kv->plan = kv->arrived + SISO_KV_JOINS;
+        ok = ok && hipMalloc((void **)&kv->parts, SISO_KV_PARTS * sizeof(float)) == hipSuccess;
         ok = ok && hipDeviceSynchronize() == hipSuccess;
     }
     if (!ok) {

@@ -22,8 +22,10 @@ struct KvAttend {
     int window;        // 0 = all
     bf16_t *out;
     float *lse;
-    float *parts;       // [2 * workgroups]: sums [32][DP], then maximum and sum of each row
-    unsigned *arrived;  // [workgroups]: parts of a tile that are there, by the first workgroup that works on it; zeros between calls
+    float *parts;       // [2 * KV_STRETCHES]: sums [32][DP], then maximum and sum of each row
+    unsigned *arrived;  // [2 * KV_STRETCHES]: parts of a tile that are there, by the number of its first; zeros between calls
+    struct KvPlan *plan;
+    long item0, items;  // of this launch the first; how many there may be
 };
 
 struct KvTile {
@@ -99,17 +101,27 @@ __device__ __forceinline__ void kv_finish(const KvAttend &a, const KvTile &t, in
     if (d == 0 && a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f;
 }
 
-// Sequences of few rows of work (at most KV_FEW: one token, a draft's few).  Each has tiles of 32 rows for each of its kv heads, each tile the
-// same number of units of KS positions (32, or 64 of 64 elements); all units of all sequences, one after the other, are cut into as many equal stretches as there are
-// workgroups.  So every workgroup has the same to do, whatever the lengths are, and nobody has to know them beforehand.
+// Sequences of few rows of work (at most KV_FEW: one token, a draft's few).  Each has tiles of 32 rows for each of its kv heads, each tile a
+// number of units of KS positions.  The units of all tiles together, on the device, say how many make a stretch: KV_STRETCHES of them hold
+// them all.  A tile of more is cut into stretches, each a workgroup's: nobody has more to do than one stretch, whatever the lengths
+// are, and nobody but the device knows them.  Tiles and stretches are at most tiles + KV_STRETCHES items, at most 2 * KV_STRETCHES of them
+// parts of a tile that is cut.
 #define KV_FEW 128
+#define KV_STRETCHES 1024
 #define KV_LEAST 4  // units of a stretch, at least: one for each wave
+#define KV_ENOUGH 32 // units that are worth being joined
+#define KV_FULL 256  // workgroups
+#define KV_PLAN_CHUNKS 1024  // 65,535 sequences, 64 each
+struct KvPlan {  // more than 64 sequences: made by a launch of its own
+    unsigned stretch;
+    unsigned items[KV_PLAN_CHUNKS], parts[KV_PLAN_CHUNKS];  // before each 64 sequences
+};
+static_assert(sizeof(KvPlan) <= SISO_KV_PLAN_BYTES, "room for the plan");
+
 template <int KS>
 struct KvFew {
-    int chunk;            // the first of 64 sequences that this wave holds, one a lane
     int first, rows, length;  // of this lane's sequence
-    int tiles, range;     // its tiles (of all kv heads; 0: not one of these sequences) and the units of each
-    unsigned upto, mine;  // units before the next sequence, its own
+    int tiles, range;         // its tiles (of all kv heads; 0: not one of these sequences) and the units of each
     __device__ __forceinline__ static int range_of(const KvAttend &a, int start, int length, int &from) {
         from = kv_window_from(a, start) & ~(KS - 1);
         const int r = (length - from + KS - 1) / KS;
@@ -127,76 +139,89 @@ struct KvFew {
         tiles = ((rows * a.group + 31) >> 5) * a.pool.kv_heads;
         range = range_of(a, s.start, length, from);
     }
-    // Units are numbered so that a tile's are a multiple of `whole`.
-    __device__ __forceinline__ void number(const KvAttend &a, unsigned before, int whole) {
+    __device__ __forceinline__ u64 units() const { return (u64)tiles * (unsigned)range; }
+    // Units of a stretch, from how many there are of units and tiles: KV_ENOUGH of them at least, less only where that would not
+    // fill the chip, and so many that there are no more than KV_STRETCHES, nor than the launch has workgroups for.
+    __device__ __forceinline__ static unsigned stretch_of(const KvAttend &a, u64 all, u64 all_tiles) {
+        const u64 room = a.items - all_tiles < KV_STRETCHES ? a.items - all_tiles : KV_STRETCHES;
+        if (room == 0) return 0x7FFFFFFFu;
+        unsigned s = all < KV_FULL * KV_ENOUGH ? (unsigned)all / KV_FULL : KV_ENOUGH;
+        s = s > KV_LEAST ? s : KV_LEAST;
+        const unsigned most = (unsigned)((all + room - 1) / room);
+        return s > most ? s : most;
+    }
+    __device__ __forceinline__ unsigned cuts(unsigned stretch) const { return tiles ? ((unsigned)range + stretch - 1) / stretch : 0; }
+    __device__ __forceinline__ static unsigned running_sum(unsigned v) {
         const int lane = threadIdx.x & 63;
-        mine = tiles * (whole > 1 ? (range + whole - 1) / whole * whole : range);
-        upto = mine;
-        if (a.batch.n > 1)
 #pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const unsigned x = __shfl_up(upto, off);
-                if (lane >= off) upto += x;
-            }
-        else upto = __builtin_amdgcn_readfirstlane(upto);
-        upto += before;
-    }
-    __device__ __forceinline__ unsigned end() const { return __builtin_amdgcn_readlane(upto, 63); }
-    // Where tiles are few, a stretch lies within one of them: so many units that no more than `most` stretches come of it.  Else a
-    // tile may end within a stretch.  Returns all units, sets their number in a stretch and what a tile's are a multiple of.
-    __device__ __forceinline__ unsigned plan(const KvAttend &a, unsigned most, unsigned &stretch, int &whole) {
-        chunk = 0;
-        load(a, threadIdx.x & 63);
-        unsigned all_tiles, all;
-        if (a.batch.n == 1) {
-            all_tiles = __builtin_amdgcn_readfirstlane(tiles);
-            all = all_tiles * __builtin_amdgcn_readfirstlane(range);
-        } else {
-            unsigned t = tiles, u = tiles * range;
-            if (a.batch.n > 64) {
-                KvFew other;
-#pragma unroll 4
-                for (int b = 64 + (threadIdx.x & 63); b < a.batch.n; b += 64) {
-                    other.load(a, b);
-                    t += other.tiles;
-                    u += other.tiles * other.range;
-                }
-            }
-            auto add = [](unsigned x, unsigned y) __attribute__((always_inline)) { return x + y; };
-            all_tiles = __builtin_amdgcn_readfirstlane(wave_fold(t, add));
-            all = __builtin_amdgcn_readfirstlane(wave_fold(u, add));
+        for (int off = 1; off < 64; off <<= 1) {
+            const unsigned x = __shfl_up(v, off);
+            if (lane >= off) v += x;
         }
-        const bool apart = 2 * all_tiles <= most;
-        const unsigned ways = apart ? most - all_tiles : most;
-        stretch = (all + ways - 1) / ways;
-        if (stretch < KV_LEAST) stretch = KV_LEAST;
-        stretch = __builtin_amdgcn_readfirstlane(stretch);
-        whole = apart ? stretch : 1;
-        number(a, 0, whole);
-        return a.batch.n == 1 ? end() : apart ? most * stretch : all;  // (apart: the stretches beyond the last find nothing)
-    }
-    // The sequence that unit x is of, or -1; `before`: the units before it.
-    __device__ __forceinline__ int find(const KvAttend &a, unsigned x, int whole, unsigned &before, KvSequence &s) {
-        while (end() <= x) {
-            if (chunk + 64 >= a.batch.n) return -1;
-            const unsigned so_far = end();
-            chunk += 64;
-            load(a, chunk + (threadIdx.x & 63));
-            number(a, so_far, whole);
-        }
-        const int at = __ffsll((long long)__ballot(upto > x)) - 1;
-        before = __builtin_amdgcn_readlane(upto - mine, at);
-        s.b = chunk + at;
-        s.first = __builtin_amdgcn_readlane(first, at);
-        s.rows = __builtin_amdgcn_readlane(rows, at);
-        s.length = __builtin_amdgcn_readlane(length, at);
-        s.start = s.length - s.rows;
-        return s.b;
+        return v;
     }
 };
-// One workgroup for a stretch of units; its four waves take every fourth unit of a tile, each with sums of its own, which are
+__device__ __forceinline__ u64 kv_wave_sum(u64 v) {
+    return wave_fold(v, [](u64 a, u64 b) __attribute__((always_inline)) { return a + b; });
+}
+
+// What every workgroup of k_kv_attend_few has to know of all sequences, where they are more than a wave takes in.
+template <int KS>
+__global__ __launch_bounds__(1024) void k_kv_plan(KvAttend a) {
+    __shared__ u64 sums[32];
+    __shared__ unsigned items[KV_PLAN_CHUNKS], parts[KV_PLAN_CHUNKS], waves[2][16];
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6, chunks = (a.batch.n + 63) / 64;
+    KvFew<KS> few;
+    u64 all = 0, all_tiles = 0;
+    for (int b = t; b < a.batch.n; b += 1024) {
+        few.load(a, b);
+        all += few.units();
+        all_tiles += few.tiles;
+    }
+    all = kv_wave_sum(all);
+    all_tiles = kv_wave_sum(all_tiles);
+    if (lane == 0) {
+        sums[w] = all;
+        sums[16 + w] = all_tiles;
+    }
+    __syncthreads();
+    all = all_tiles = 0;
+    for (int i = 0; i < 16; ++i) {
+        all += sums[i];
+        all_tiles += sums[16 + i];
+    }
+    const unsigned stretch = KvFew<KS>::stretch_of(a, all, all_tiles);
+    for (int c = w; c < chunks; c += 16) {
+        few.load(a, 64 * c + lane);
+        const unsigned cuts = few.cuts(stretch), mine = few.tiles * cuts;
+        const u64 both = kv_wave_sum(((u64)mine << 32) | (cuts > 1 ? mine : 0u));
+        if (lane == 0) {
+            items[c] = (unsigned)(both >> 32);
+            parts[c] = (unsigned)both;
+        }
+    }
+    __syncthreads();
+    const unsigned mine = t < chunks ? items[t] : 0, my_parts = t < chunks ? parts[t] : 0;
+    unsigned upto = KvFew<KS>::running_sum(mine), upto_parts = KvFew<KS>::running_sum(my_parts);
+    if (lane == 63) {
+        waves[0][w] = upto;
+        waves[1][w] = upto_parts;
+    }
+    __syncthreads();
+    for (int i = 0; i < w; ++i) {
+        upto += waves[0][i];
+        upto_parts += waves[1][i];
+    }
+    if (t < chunks) {
+        a.plan->items[t] = upto - mine;
+        a.plan->parts[t] = upto_parts - my_parts;
+    }
+    if (t == 0) a.plan->stretch = stretch;
+}
+
+// One workgroup for a stretch of a tile's units; its four waves take every fourth of them, each with sums of its own, which are
 // joined through LDS in the order of the waves.  Keys and values go straight from memory to registers: no wave reads what another does.
-// A tile that several workgroups have a part of is finished by the one that is done last, from all parts, in their order.
+// A tile that is cut is finished by the workgroup that is done last, from all parts, in their order.
 // KS: positions of a step.  A wave has one step's operands on their way while it works on the last one's.
 constexpr int kv_step(int dp) { return dp <= 64 ? 64 : 32; }
 template <int DP, bool FP8>
@@ -210,30 +235,63 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
     __shared__ float sh_m[4 * 32], sh_l[4 * 32];
     __shared__ int sh_last;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
-    KvFew<KS> few;
-    unsigned stretch;
-    int whole;
-    const unsigned all = few.plan(a, gridDim.x, stretch, whole);
-    unsigned unit = blockIdx.x * stretch;
-    const unsigned last_unit = unit + stretch < all ? unit + stretch : all;
-#pragma unroll 1
-    while (unit < last_unit) {
     KvTile t;
-    unsigned before;
-    if (few.find(a, unit, whole, before, t.s) < 0) return;
-    int base;
-    int range = KvFew<KS>::range_of(a, t.s.start, t.s.length, base);
-    if (whole > 1) range = (range + whole - 1) / whole * whole;
-    range = __builtin_amdgcn_readfirstlane(range);
-    const int which = __builtin_amdgcn_readfirstlane((unit - before) / (unsigned)range), unit0 = unit - before - which * range;
-    const int units = last_unit - unit < (unsigned)(range - unit0) ? last_unit - unit : range - unit0;
-    const int tile = __builtin_amdgcn_readfirstlane(which / a.pool.kv_heads), head = which - tile * a.pool.kv_heads;
-    kv_tile(a, tile * 32, 32, t);
-    const unsigned tile_unit = unit - unit0;
-    const int first_workgroup = __builtin_amdgcn_readfirstlane(tile_unit / stretch), count = __builtin_amdgcn_readfirstlane((tile_unit + range - 1) / stretch) - first_workgroup + 1;
-    int from = base + KS * unit0, to = from + KS * units;
-    if (from < (t.lo & ~(KS - 1))) from = t.lo & ~(KS - 1);
-    if (to > t.hi) to = t.hi;
+    int head, from, to, piece, count;  // of the tile's pieces
+    unsigned first_part;               // of the tile
+    {
+        const unsigned item = (unsigned)(a.item0 + blockIdx.x);
+        KvFew<KS> few;
+        unsigned stretch, items_before = 0, parts_before = 0;
+        int chunk = 0;
+        if (a.batch.n <= 64) {
+            few.load(a, lane);
+            u64 all = few.units(), all_tiles = few.tiles;
+            if (a.batch.n > 1) {
+                all = kv_wave_sum(all);
+                all_tiles = kv_wave_sum(all_tiles);
+            }
+            stretch = __builtin_amdgcn_readfirstlane(KvFew<KS>::stretch_of(a, all, all_tiles));
+        } else {  // the last 64 with no more items before them than this one
+            int count = (a.batch.n + 63) / 64;
+            while (count > 1) {
+                const int step = (count + 63) / 64;
+                const bool before = lane * step < count && a.plan->items[chunk + lane * step] <= item;
+                const int k = __popcll(__ballot(before)) - 1;  // (the first is 0)
+                chunk += k * step;
+                count = count - k * step < step ? count - k * step : step;
+            }
+            stretch = __builtin_amdgcn_readfirstlane(a.plan->stretch);
+            items_before = __builtin_amdgcn_readfirstlane(a.plan->items[chunk]);
+            parts_before = __builtin_amdgcn_readfirstlane(a.plan->parts[chunk]);
+            few.load(a, 64 * chunk + lane);
+        }
+        const unsigned cuts = few.cuts(stretch), mine = few.tiles * cuts, my_parts = cuts > 1 ? mine : 0;
+        const unsigned upto = items_before + (a.batch.n > 1 ? KvFew<KS>::running_sum(mine) : mine);
+        const unsigned upto_parts = parts_before + (a.batch.n > 1 ? KvFew<KS>::running_sum(my_parts) : my_parts);
+        const u64 over = __ballot(upto > item);
+        if (over == 0) return;  // (there are not as many items)
+        const int at = __ffsll((long long)over) - 1;
+        t.s.b = 64 * chunk + at;
+        t.s.first = __builtin_amdgcn_readlane(few.first, at);
+        t.s.rows = __builtin_amdgcn_readlane(few.rows, at);
+        t.s.length = __builtin_amdgcn_readlane(few.length, at);
+        t.s.start = t.s.length - t.s.rows;
+        count = __builtin_amdgcn_readlane(cuts, at);
+        const unsigned in = item - __builtin_amdgcn_readlane(upto - mine, at);
+        // heads first, then pieces: neighbours read the same pages
+        const unsigned rest = __builtin_amdgcn_readfirstlane(in / (unsigned)a.pool.kv_heads);
+        head = in - rest * a.pool.kv_heads;
+        const unsigned tile = __builtin_amdgcn_readfirstlane(rest / (unsigned)count);
+        piece = rest - tile * count;
+        first_part = __builtin_amdgcn_readlane(upto_parts - my_parts, at) + (tile * a.pool.kv_heads + head) * count;
+        kv_tile(a, tile * 32, 32, t);
+        int base;
+        KvFew<KS>::range_of(a, t.s.start, t.s.length, base);
+        from = base + KS * (int)(piece * stretch);
+        to = from + KS * (int)stretch;
+        if (from < (t.lo & ~(KS - 1))) from = t.lo & ~(KS - 1);
+        if (to > t.hi || piece == count - 1) to = t.hi;
+    }
 
     // this lane's row (of both halves) as the operand Q^T
     const int row = t.row0 + n, token = row / a.group, qh = head * a.group + row % a.group;
@@ -481,8 +539,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
         for (int g = 0; g < 4; ++g)
             *(float4 *)(sh + (w * 32 + n) * RS + 32 * u + 8 * g + 4 * h) = make_float4(o[u][4 * g], o[u][4 * g + 1], o[u][4 * g + 2], o[u][4 * g + 3]);
     __syncthreads();
-    // (of a tile's parts only the first begins with it, and of a workgroup's only one does not)
-    float *part = a.parts + (size_t)(2 * blockIdx.x + (unit0 == 0)) * KV_PART(DP);
+    float *part = a.parts + (size_t)(first_part + piece) * KV_PART(DP);
     for (int i = threadIdx.x; i < t.rows * (DP / 4); i += 256) {
         const int r = i / (DP / 4), d = i % (DP / 4) * 4;
         float mj[4], top = -INFINITY;
@@ -506,13 +563,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's numbers are where all workgroups see them
         __syncthreads();
         if (threadIdx.x == 0) {
-            sh_last = atomicAdd(a.arrived + first_workgroup, 1u) == (unsigned)(count - 1);
-            if (sh_last) a.arrived[first_workgroup] = 0;  // (for the next call: nobody else comes)
+            sh_last = atomicAdd(a.arrived + first_part, 1u) == (unsigned)(count - 1);
+            if (sh_last) a.arrived[first_part] = 0;  // (for the next call: nobody else comes)
         }
         __syncthreads();
         if (sh_last) {
-            const float *parts = a.parts + (size_t)2 * first_workgroup * KV_PART(DP);
-            auto part_of = [&](int s) { return parts + (size_t)(2 * s + (s == 0)) * KV_PART(DP); };
+            const float *parts = a.parts + (size_t)first_part * KV_PART(DP);
+            auto part_of = [&](int s) { return parts + (size_t)s * KV_PART(DP); };
             // few rows leave threads idle: these take every second, fourth or eighth part
             const int work = t.rows * (DP / 4), across = work > 128 ? 1 : work > 64 ? 2 : work > 32 ? 4 : 8, wide = 256 / across;
             const int mine = threadIdx.x & (wide - 1), lead = threadIdx.x / wide;
@@ -560,9 +617,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
                 if (across > 1) break;
             }
         }
-    }
-    unit += units;
-    __syncthreads();
     }
 }
 
@@ -941,8 +995,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) 
     }
 }
 
-// Workgroups that run at once: two on each of 256 compute units, one where a wave needs more than half of the registers.
-static int kv_few_workgroups(int dp) { return dp <= 128 ? 512 : 256; }
+// Workgroups that run at once on 256 compute units.
 static int kv_chunk_workgroups(int dp) { return dp == 64 ? 768 : 256; }
 
 template <int DP, bool FP8>
@@ -951,7 +1004,7 @@ static int attend_chunks(siso_kv *kv, KvAttend &a, int few) {
     KvPieces p;
     p.few = few;
     p.slots = kv_slots_before(a.batch.rows, a.batch.n, a.group, C::ROWS == 256 ? 8 : 7, 1);
-    const long tiles = p.slots * kv->kv_heads, room = (long)(kv->parts_floats / KV_CHUNK_PART(C::ROWS, DP));
+    const long tiles = p.slots * kv->kv_heads, room = (long)(SISO_KV_PARTS / KV_CHUNK_PART(C::ROWS, DP));
     long ways = tiles <= kv_chunk_workgroups(DP) / 2 ? kv_chunk_workgroups(DP) / tiles : 1;
     if (ways > room / tiles) ways = room / tiles;
     if (ways > 64) ways = 64;
@@ -979,20 +1032,19 @@ static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
         if (rc != SISO_OK || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
     }
     constexpr int KS = kv_step(DP);
-    const long tiles = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads, units = tiles * (max_length / KS + 2);
-    const long enough = (units + KV_LEAST - 1) / KV_LEAST;
-    const dim3 grid((unsigned)(enough < kv_few_workgroups(DP) ? enough : kv_few_workgroups(DP)));
-    // (a launch counts its units in 32 bits: sequences that could have more go in several)
-    const long most = (long)(KV_FEW / 32) * kv->kv_heads * (a.batch.most / KS + 2), step = (1L << 30) / most;
-    if (step < 1) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: %d kv heads of sequences of %d tokens", kv->kv_heads, a.batch.most);
-    const int n = a.batch.n;
-    for (long b0 = 0; b0 < n; b0 += step) {
-        a.batch.n = (int)(n - b0 < step ? n - b0 : step);
+    const long tiles = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads, cuts = (max_length / KS + 2 + KV_LEAST - 1) / KV_LEAST;
+    const long items = tiles * cuts < tiles + KV_STRETCHES ? tiles * cuts : tiles + KV_STRETCHES, piece = 1L << 23;
+    a.items = items;
+    a.item0 = 0;
+    static_assert((size_t)2 * KV_STRETCHES * KV_PART(256) <= SISO_KV_PARTS && 2 * KV_STRETCHES <= SISO_KV_JOINS, "room for the parts");
+    if (a.batch.n > 64) {
+        hipLaunchKernelGGL(k_kv_plan<KS>, dim3(1), dim3(1024), 0, kv->stream, a);
+        KV_TRY(kv, hipGetLastError());
+    }
+    for (; a.item0 < items; a.item0 += piece) {  // (a launch has fewer than 2^32 threads)
+        const dim3 grid((unsigned)(items - a.item0 < piece ? items - a.item0 : piece));
         hipLaunchKernelGGL((k_kv_attend_few<DP, FP8>), grid, dim3(256), 0, kv->stream, a);
         KV_TRY(kv, hipGetLastError());
-        a.batch.first += a.batch.n;
-        a.batch.length += a.batch.n;
-        a.batch.pages += a.batch.n * a.batch.width;
     }
     return SISO_OK;
 }
@@ -1024,6 +1076,7 @@ extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch
     a.lse = lse;
     a.parts = kv->parts;
     a.arrived = kv->arrived;
+    a.plan = (KvPlan *)kv->plan;
     const long max_new = batch->max_new > 0 && batch->max_new < a.batch.rows ? batch->max_new : a.batch.rows;
     const long max_length = batch->max_length > 0 && batch->max_length < a.batch.most ? batch->max_length : a.batch.most;
     switch (kv->dp / 64 + (kv->dtype == SISO_FP8 ? 4 : 0)) {

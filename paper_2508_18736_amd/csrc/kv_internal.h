@@ -93,6 +93,8 @@ __device__ __forceinline__ size_t kv_scale_at(const KvPool &pool, int page, int 
 }
 #endif
 
+#define SISO_KV_PARTS ((size_t)32 << 20)  // 128 MiB
+#define SISO_KV_PLAN_BYTES 16384
 #define SISO_KV_JOINS 65536  // sequences of a batch; workgroups of an attention launch that leaves parts to be joined are fewer
 
 struct siso_kv {
@@ -104,8 +106,8 @@ struct siso_kv {
     size_t layer_bytes, layer_scales;
     u64 *counters;      // [0] page numbers that are none; behind it `arrived`
     unsigned *arrived;  // [SISO_KV_JOINS] how many parts are there of what several workgroups work on; zeros between calls
-    float *parts;  // what splits of a long axis leave for the one that joins them; see kv_attend.hip and kv_verify.hip
-    size_t parts_floats;
+    void *plan;         // [SISO_KV_PLAN_BYTES], see kv_attend.hip
+    float *parts;       // [SISO_KV_PARTS] what splits of a long axis leave for the one that joins them; see kv_attend.hip and kv_verify.hip
     char err[256];
 };
 
