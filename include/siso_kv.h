@@ -100,7 +100,8 @@ int siso_kv_read(siso_kv *kv, int layer, const siso_kv_batch *batch, int out_typ
  *     s_j = scale * <q, k_j>,   j <= P, and j > P - window if window > 0
  *     out = sum_j exp(s_j) v_j / sum_j exp(s_j),   lse = log sum_j exp(s_j)
  *   q:     device pointer, 16-bit rows, strides as for siso_kv_write.
- *   heads: a multiple of kv_heads, at most 128 of them for each (SISO_EINVAL otherwise).
+ *   heads: a multiple of kv_heads, at most 128 of them for each; rows * heads at most 2^30
+ *          (SISO_EINVAL otherwise).
  *   scale: finite.
  *   out:   device pointer, [rows][heads][head_dim], 16 bits, 16-byte aligned.
  *   lse:   device pointer, [rows][heads] floats, or NULL.

@@ -38,7 +38,7 @@ __device__ __forceinline__ int kv_window_from(const KvAttend &a, int pos) {  // 
     return a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
 }
 __device__ __forceinline__ void kv_tile(const KvAttend &a, int row0, int size, KvTile &t) {
-    const int work = t.s.rows * a.group;  // (at most 2^24 rows, 128 heads: 2^31 at most, and then not here)
+    const int work = t.s.rows * a.group;  // (2^30 at most)
     t.row0 = row0;
     t.rows = work - row0 < size ? work - row0 : size;
     const int first = t.s.start + row0 / a.group, last = t.s.start + (row0 + t.rows - 1) / a.group;
@@ -621,12 +621,18 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
 }
 
 // Sequences of more rows of work: a prompt's chunk.  One workgroup for a tile of NW * 32 rows, each wave for 32 of them over all
-// positions.  Keys and values pass through LDS in stages of KEYS positions, three of them: one is used, the next is there, the one
-// after is written while its successor is on its way from memory.  Codes become 16-bit numbers (exactly) on the way in.
+// positions, in stages of KEYS.  A wave goes through a stage in two phases with a barrier behind each: one of products, the scores of the next
+// stage and the sums of this one, and one of powers, of the next stage's scores.  Both take about as long, the one on the matrix cores, the
+// other on the vector units, and of the two waves on a SIMD unit one is always a phase behind: each has the unit that the other leaves.
+// (4,096 rows of 32 heads of 128 behind 8,193: 655 us, 1,050 TFLOP/s; in step, with one barrier a stage, both waited for the same unit: 785 us.)
+// Keys and values pass through LDS, two stages of each: keys are read a stage earlier than values.  A wave writes its share of the next ones
+// and asks for those after them in its phase of products, whose vector units are idle.  Codes become 16-bit numbers (exactly) on the way in.
 template <int DP, bool FP8>
 struct KvChunk {
-    static constexpr int NW = DP == 128 ? 8 : 4;  // waves: two on each SIMD unit of 128 elements, of 64 three workgroups of one
-    static constexpr int NT = 64 * NW, ROWS = 32 * NW, PER_SIMD = DP == 64 ? 3 : NW / 4;
+    // Waves: two on each SIMD unit.  Of 64 elements they are those of two workgroups (of one of eight waves 1,500 rows at most and windows of 1,000
+    // took 84 us, not 61; three workgroups do not have the registers: 68), of more than 128 there is room for one.
+    static constexpr int NW = DP == 128 ? 8 : 4;
+    static constexpr int NT = 64 * NW, ROWS = 32 * NW, PER_SIMD = DP <= 128 ? 2 : 1;
     static constexpr int KEYS = DP <= 192 ? 64 : 32, SUBS = KEYS / 32, BLOCKS = KEYS / 16;
     static constexpr int ES = FP8 ? 1 : 2;
     static constexpr int NS = DP / 16, NU = DP / 32;
@@ -634,9 +640,10 @@ struct KvChunk {
     static constexpr int CHUNKS = BLOCKS * BLOCK_CHUNKS;   // of a stage's keys
     static constexpr int NL = (CHUNKS + NT - 1) / NT;      // of a thread
     static constexpr int HALF = KEYS * DP * 2;             // bytes of a stage's keys in LDS
-    static constexpr int STAGE = 2 * HALF + (FP8 ? 2 * KEYS * 4 : 0);
-    static constexpr int LDS = 3 * STAGE;
-    static_assert(LDS <= 160 * 1024, "fits LDS");
+    static constexpr int SCALES = 4 * HALF;                // (8 bits) where the scales begin: of four stages, keys' and values'
+    static constexpr int FOUND = SCALES + (FP8 ? 4 * 2 * KEYS * 4 : 0);  // two words: a value that is not finite, a maximum that grew too far
+    static constexpr int LDS = FOUND + 16 + 4 * BLOCKS * 4;  // and which blocks of four stages have a page
+    static_assert(LDS <= 160 * 1024 && NT >= 2 * KEYS, "fits LDS; a thread for each scale");
 };
 #define KV_CHUNK_PART(ROWS, DP) ((size_t)(ROWS) * ((DP) + 2))
 
@@ -646,6 +653,12 @@ struct KvPieces {
     int few;   // sequences of at most so many rows of work are left to k_kv_attend_few
 };
 #define KV_PIECE_LEAST 256  // positions
+// A phase of products: operands are read so many products ahead (4: 1% slower, 8: 2%), and the work of the next stages begins behind this one.
+#define KV_AHEAD 6
+#define KV_FORWARD 4
+// What may pass a product in the compiler's order: vector and scalar arithmetic, memory reads and writes, writes to LDS; reads of LDS
+// and products may not.  (Nothing bounded, the compiler moves operands' reads to where they are waited for: 8% slower.)
+#define KV_MASK 0x276
 // The tile of a slot, of `rows` rows of work, and how its positions are cut: pieces of `per` blocks of KEYS positions from `from` on.
 template <int ROWS, int KEYS>
 __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces &p, long slot, KvTile &t, int &from, int &blocks, int &per, int &pieces) {
@@ -709,104 +722,169 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
     for (int u = 0; u < NU; ++u) o[u] = f32x16_t{};
 
     // ---- stages: pages from the table, a stage from memory to registers, from registers to LDS
+    // Every thread looks up the pages of its own chunks, a stage before it fetches them: what the scalar unit would have to work out
+    // for all of them takes longer than the products.  Stages beyond the last are fetched and written as others (at positions of the last page), and not read.
+    const int late = C::NW == 8 ? w >> 2 : 0;  // this wave is a phase behind
     u32x4_t gk[NL], gv[NL];
     float gs = 0.f;
-    int entry[BLOCKS];  // what the table says of the stage that is fetched next
-    auto look_up = [&](int at) {
-#pragma unroll
-        for (int blk = 0; blk < BLOCKS; ++blk) entry[blk] = kv_page_entry(a.pool, a.batch, t.s.b, at + 16 * blk < t.hi ? at + 16 * blk : t.hi - 1);
+    int entry[NL], scale_entry = 0;       // what the table says of the stage whose keys are fetched next
+    const char *k_at[NL], *v_at[NL];      // where this thread's chunks of its keys are; of the values of the one before
+    unsigned k_held = 0, v_held = 0, gv_held = 0;  // a bit for each of them that is in a page of the cache; of those in gv
+    // What hardly ever is, is only looked for, in `odd`, and the tile done again with care if it is found: pages that are none, and values that
+    // are not finite (nothing times an infinity is NaN, so they must not reach the rows that do not see them).
+    bool careful = false;
+    unsigned odd = 0;
+    const int *const table = a.batch.pages + (long)t.s.b * a.batch.width;
+    const long page_bytes = ((long)a.pool.kv_heads << a.pool.shift) * DP * C::ES, head_bytes = ((long)head << a.pool.shift) * DP * C::ES;
+    const int in_page = (1 << a.pool.shift) - 1;
+    auto position = [&](int stage, int blk) {
+        const int p = first + stage * KEYS + 16 * blk;
+        return p < t.hi ? p : (t.hi - 1) & ~15;
     };
-    auto fetch = [&](int at) {  // returns a bit for each block that has a page
-        size_t base[BLOCKS];
-        int page[BLOCKS], is_page = 0;
+    auto look_up = [&](int stage) {
 #pragma unroll
-        for (int blk = 0; blk < BLOCKS; ++blk) {
-            is_page |= kv_is_page(a.pool, entry[blk]) ? 1 << blk : 0;
-            page[blk] = kv_is_page(a.pool, entry[blk]) ? entry[blk] : 0;
-            base[blk] = kv_block_at(a.pool, page[blk], head, at + 16 * blk) * C::ES;
-        }
+        for (int i = 0; i < NL; ++i) entry[i] = table[position(stage, (threadIdx.x + C::NT * i) / C::BLOCK_CHUNKS % BLOCKS) >> a.pool.shift];
+        if constexpr (FP8) scale_entry = table[position(stage, (threadIdx.x & (KEYS - 1)) >> 4) >> a.pool.shift];
+    };
+    auto fetch_keys = [&](int stage) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            const int c = threadIdx.x + C::NT * i, blk = c / C::BLOCK_CHUNKS;
-            size_t off = base[0];
-#pragma unroll
-            for (int k = 1; k < BLOCKS; ++k) off = blk == k ? base[k] : off;
-            off += (size_t)(c % C::BLOCK_CHUNKS) * 16;
-            if (C::CHUNKS % C::NT == 0 || c < C::CHUNKS) {
-                gk[i] = *(const u32x4_t *)(a.pool.k + off);
-                gv[i] = *(const u32x4_t *)(a.pool.v + off);
-            }
+            const int c = threadIdx.x + C::NT * i, at = position(stage, c / C::BLOCK_CHUNKS % BLOCKS);
+            const bool held = kv_is_page(a.pool, entry[i]);
+            k_held = (k_held & ~(1u << i)) | (unsigned)held << i;
+            odd |= held ? 0u : 0x8000u;
+            const long off = (held ? entry[i] : 0) * page_bytes + head_bytes + ((at & in_page) >> 4) * (C::BLOCK_CHUNKS * 16) + c % C::BLOCK_CHUNKS * 16;
+            gk[i] = *(const u32x4_t *)(a.pool.k + off);
+            k_at[i] = a.pool.v + off;
         }
-        if (FP8 && threadIdx.x < 2 * KEYS) {
-            const int key = threadIdx.x & (KEYS - 1);
-            int pg = page[0];
-#pragma unroll
-            for (int k = 1; k < BLOCKS; ++k) pg = key >> 4 == k ? page[k] : pg;
-            const float *scales = threadIdx.x < KEYS ? a.pool.ks : a.pool.vs;
-            gs = scales[kv_scale_at(a.pool, pg, head, at + (key & ~15)) + (key & 15)];
+        if constexpr (FP8) {
+            const int key = threadIdx.x & (KEYS - 1), at = position(stage, key >> 4);
+            const bool held = kv_is_page(a.pool, scale_entry);
+            const float *scales = threadIdx.x & KEYS ? a.pool.vs : a.pool.ks;
+            gs = scales[(((long)(held ? scale_entry : 0) * a.pool.kv_heads + head) << a.pool.shift) + (at & in_page) + (key & 15)];
+            gs = held ? gs : 0.f;
         }
-        return is_page;
     };
-    auto put = [&](int buffer) {
-        char *to = lds + buffer * C::STAGE;
+    auto fetch_values = [&]() {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) gv[i] = *(const u32x4_t *)v_at[i];
+        gv_held = v_held;
+    };
+    auto next = [&]() {  // the stage whose keys are fetched becomes that whose values are
+#pragma unroll
+        for (int i = 0; i < NL; ++i) v_at[i] = k_at[i];
+        v_held = k_held;
+    };
+    int *const found = (int *)(lds + C::FOUND);
+    int *const held = found + 4;  // [4][BLOCKS]: of four stages the blocks that have a page
+    auto put_keys = [&](int stage) __attribute__((always_inline)) {
+        char *k = lds + (stage & 1) * C::HALF;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int c = threadIdx.x + C::NT * i, blk = c / C::BLOCK_CHUNKS, r = c % C::BLOCK_CHUNKS;
             if (!(C::CHUNKS % C::NT == 0 || c < C::CHUNKS)) continue;
             if constexpr (FP8) {
-                // K: chunk (2 t + h) of 16 codes and a token; two operands of 8.  V: [h][dimension / 64][32] of two operands.
-                const int kc = r >> 4, key = r & 15, vh = r / (DP / 2), vu = r % (DP / 2) >> 5, vm = r & 31;
-                const int even = 2 * (2 * (kc >> 1)) + (kc & 1);
-                *(bf16x8_t *)(to + blk * 32 * DP + (even * 16 + key) * 16) = kv_codes_bf16(gk[i][0], gk[i][1]);
-                *(bf16x8_t *)(to + blk * 32 * DP + ((even + 2) * 16 + key) * 16) = kv_codes_bf16(gk[i][2], gk[i][3]);
-                *(bf16x8_t *)(to + C::HALF + blk * 32 * DP + (vh * DP + 64 * vu + vm) * 16) = kv_codes_bf16(gv[i][0], gv[i][1]);
-                *(bf16x8_t *)(to + C::HALF + blk * 32 * DP + (vh * DP + 64 * vu + 32 + vm) * 16) = kv_codes_bf16(gv[i][2], gv[i][3]);
-            } else {
-                *(u32x4_t *)(to + c * 16) = gk[i];
-                *(u32x4_t *)(to + C::HALF + c * 16) = gv[i];
-            }
+                // chunk (2 t + h) of 16 codes and a token; two operands of 8
+                const int kc = r >> 4, key = r & 15, even = 2 * (2 * (kc >> 1)) + (kc & 1);
+                *(bf16x8_t *)(k + blk * 32 * DP + (even * 16 + key) * 16) = kv_codes_bf16(gk[i][0], gk[i][1]);
+                *(bf16x8_t *)(k + blk * 32 * DP + ((even + 2) * 16 + key) * 16) = kv_codes_bf16(gk[i][2], gk[i][3]);
+            } else *(u32x4_t *)(k + c * 16) = gk[i];
         }
-        if (FP8 && threadIdx.x < 2 * KEYS) *(float *)(to + 2 * C::HALF + threadIdx.x * 4) = gs;
+        if (FP8 && (C::NT == 2 * KEYS || threadIdx.x < 2 * KEYS)) ((float *)(lds + C::SCALES))[(stage & 3) * 2 * KEYS + threadIdx.x] = gs;
+    };
+    auto put_values = [&](int stage) __attribute__((always_inline)) {
+        char *v = lds + (2 + (stage & 1)) * C::HALF;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int c = threadIdx.x + C::NT * i, blk = c / C::BLOCK_CHUNKS, r = c % C::BLOCK_CHUNKS;
+            if constexpr (!FP8)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) odd |= (gv[i][k] & 0x7F807F80u) + 0x00800080u;  // (the top bit of a half: its exponent is all ones)
+            if (!(C::CHUNKS % C::NT == 0 || c < C::CHUNKS)) continue;
+            if constexpr (FP8) {
+                // [h][dimension / 64][32] of two operands
+                const int vh = r / (DP / 2), vu = r % (DP / 2) >> 5, vm = r & 31;
+                *(bf16x8_t *)(v + blk * 32 * DP + (vh * DP + 64 * vu + vm) * 16) = kv_codes_bf16(gv[i][0], gv[i][1]);
+                *(bf16x8_t *)(v + blk * 32 * DP + (vh * DP + 64 * vu + 32 + vm) * 16) = kv_codes_bf16(gv[i][2], gv[i][3]);
+            } else *(u32x4_t *)(v + c * 16) = gv[i];
+        }
+    };
+    auto take_care = [&](int stage) {  // before these: of the stage whose keys are put, which blocks have a page; values that are numbers only
+#pragma unroll 1
+        for (int i = 0; i < NL; ++i) {
+            const int c = threadIdx.x + C::NT * i, blk = c / C::BLOCK_CHUNKS;
+            if (c >= C::CHUNKS || c % C::BLOCK_CHUNKS != 0) continue;
+            held[(stage & 3) * BLOCKS + blk] = k_held >> i & 1;
+            if (!(k_held >> i & 1) && stage < stages) atomicAdd(a.pool.bad, 1ull);
+        }
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                unsigned x = gv_held >> i & 1 ? gv[i][c] : 0u;
+                if (!FP8 && (x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
+                if (!FP8 && (x & 0x7F800000u) == 0x7F800000u) x &= 0xFFFFu;
+                gv[i][c] = x;
+            }
     };
 
     // ---- a stage's work
-    auto scaled = [&](const char *scales, f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
+    auto keys_at = [&](int stage, int sub, int i) { return lds + (stage & 1) * C::HALF + (lane >> 4 & 1) * 32 * DP + h * 256 + (lane & 15) * 16 + sub * 64 * DP + i * 512; };
+    auto values_at = [&](int stage, int blk, int u) { return lds + (2 + (stage & 1)) * C::HALF + blk * 32 * DP + (h * DP + 32 * u + n) * 16; };
+    auto scaled = [&](int stage, int which, f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
         if constexpr (FP8)
 #pragma unroll
             for (int g = 0; g < 4 * SUBS; ++g) {
-                const float4 x = *(const float4 *)(scales + (8 * g + 4 * h) * 4);
+                const float4 x = *(const float4 *)((const float *)(lds + C::SCALES) + ((stage & 3) * 2 + which) * KEYS + 8 * g + 4 * h);
                 s[g >> 2][4 * (g & 3)] *= x.x;
                 s[g >> 2][4 * (g & 3) + 1] *= x.y;
                 s[g >> 2][4 * (g & 3) + 2] *= x.z;
                 s[g >> 2][4 * (g & 3) + 3] *= x.w;
             }
     };
-    auto scores = [&](const char *stage, f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
-        const char *k = stage + (lane >> 4 & 1) * 32 * DP + h * 256 + (lane & 15) * 16;
+    auto scores = [&](int stage, f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
             s[sub] = f32x16_t{};
-            __builtin_amdgcn_sched_barrier(0);  // (operands of one 32 at a time: more do not fit)
 #pragma unroll
             for (int i = 0; i < NS; ++i)
-                s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t *)(k + sub * 64 * DP + i * 512), kv_as_bf16(qx[i]), s[sub], 0, 0, 0);
+                s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t *)keys_at(stage, sub, i), kv_as_bf16(qx[i]), s[sub], 0, 0, 0);
         }
-        scaled(stage + 2 * C::HALF, s);
     };
-    // A maximum that grows by less than 2^8 stays as it is: powers up to 2^8 lose nothing, and the sums need not be brought down.
-    auto powers = [&](f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
-        __builtin_amdgcn_sched_barrier(0);
+    auto add_values = [&](int stage, const bf16x8_t (&pf)[BLOCKS]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int blk = 0; blk < BLOCKS; ++blk)
+#pragma unroll
+            for (int u = 0; u < NU; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t *)values_at(stage, blk, u), pf[blk], o[u], 0, 0, 0);
+    };
+    // A stage's phase of powers: its scores become operands of the products with its values.  Rows are weighed against the maximum of the first
+    // stage in which they see something, as long as they can be (see below).
+    bf16x8_t pf[BLOCKS];
+    float peak = -INFINITY;
+    auto weigh = [&](int stage, f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {
+        const int at = first + stage * KEYS;
+        const bool edge = at + KEYS > mine.all_hi || at < mine.all_lo || careful;
+        unsigned seen[SUBS];
+        scaled(stage, 0, s);
+        if (edge) {
+            const u64 bits = careful ? __ballot(held[(stage & 3) * BLOCKS + (lane & (BLOCKS - 1))] != 0) : ~0ull;  // (bit `blk` is block blk's)
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub) {
+                seen[sub] = 0;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int p = at + 32 * sub + 8 * (r >> 2) + 4 * h + (r & 3);
+                    if (p <= pos && (a.window == 0 || p > pos - a.window) && (bits >> (2 * sub + (r >> 3)) & 1)) seen[sub] |= 1u << r;
+                    s[sub][r] = seen[sub] >> r & 1 ? s[sub][r] : -INFINITY;
+                }
+            }
+        }
         float top = s[0][0];
 #pragma unroll
         for (int r = 1; r < 16 * SUBS; ++r) top = fmaxf(top, s[r >> 4][r & 15]);
         top = kv_both_halves_max(top);
-        if (__ballot((top - m) * a.scale > 8.f) != 0) {
-            const float now = fmaxf(m, top), down = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - now) * a.scale);
-            l *= down;
-#pragma unroll
-            for (int u = 0; u < NU; ++u) o[u] *= down;
-            m = now;
-        }
+        peak = fmaxf(peak, top);
+        m = m == -INFINITY ? top : m;
         const float base = m == -INFINITY ? 0.f : m * a.scale;
         float sum = 0.f;
 #pragma unroll
@@ -815,123 +893,136 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
             sum += s[r >> 4][r & 15];
         }
         l += sum;
-    };
-    auto values_at = [&](const char *stage, int blk, int u) { return stage + C::HALF + blk * 32 * DP + (h * DP + 32 * u + n) * 16; };
-    auto step = [&](const char *stage) __attribute__((always_inline)) {
-        f32x16_t s[SUBS];
-        scores(stage, s);
-        powers(s);
-        scaled(stage + 2 * C::HALF + KEYS * 4, s);
-#pragma unroll
-        for (int blk = 0; blk < BLOCKS; ++blk) {
-            if (blk % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-            bf16x8_t pf;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) pf[r] = (__bf16)s[blk >> 1][8 * (blk & 1) + r];
-#pragma unroll
-            for (int u = 0; u < NU; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t *)values_at(stage, blk, u), pf, o[u], 0, 0, 0);
-        }
-    };
-    // The same where some rows do not see all positions, or infinities may stand where nobody sees them (see k_kv_attend_few).
-    auto step_edge = [&](const char *stage, int at, int is_page) __attribute__((always_inline)) {
-        f32x16_t s[SUBS];
-        unsigned seen[SUBS];
-        scores(stage, s);
-#pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub) {
-            seen[sub] = 0;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int p = at + 32 * sub + 8 * (r >> 2) + 4 * h + (r & 3);
-                if (p <= pos && (a.window == 0 || p > pos - a.window) && (is_page >> (2 * sub + (r >> 3)) & 1)) seen[sub] |= 1u << r;
-                s[sub][r] = seen[sub] >> r & 1 ? s[sub][r] : -INFINITY;
-            }
-        }
-        powers(s);
-        scaled(stage + 2 * C::HALF + KEYS * 4, s);
-        if constexpr (FP8)
+        scaled(stage, 1, s);
+        if (FP8 && edge)  // (the scale of what nobody sees may be NaN)
 #pragma unroll
             for (int r = 0; r < 16 * SUBS; ++r) s[r >> 4][r & 15] = seen[r >> 4] >> (r & 15) & 1 ? s[r >> 4][r & 15] : 0.f;
 #pragma unroll
-        for (int blk = 0; blk < BLOCKS; ++blk) {
-            __builtin_amdgcn_sched_barrier(0);
-            bf16x8_t pf;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) pf[r] = (__bf16)s[blk >> 1][8 * (blk & 1) + r];
-            bool odd = false;
-            if constexpr (!FP8)
-#pragma unroll
-                for (int u = 0; u < NU; ++u) {
-                    const u32x4_t x = *(const u32x4_t *)values_at(stage, blk, u);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) odd = odd || kv_not_finite(x[c]);
-                }
-            if (__ballot(odd) != 0) {
-#pragma unroll 1
-                for (int slot = 0; slot < 16; ++slot) {
-                    const unsigned half = slot >> 3 == h ? (slot & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
-                    const u64 seen_by = __ballot(seen[blk >> 1] >> (8 * (blk & 1) + (slot & 7)) & 1);
-                    const bool sees = seen_by >> (n + 32 * (slot >> 3)) & 1;
-#pragma unroll
-                    for (int u = 0; u < NU; ++u) {
-                        u32x4_t x = *(const u32x4_t *)values_at(stage, blk, u);
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            x[c] &= c == (slot & 7) >> 1 ? half : 0u;
-                            x[c] = kv_not_finite(x[c]) ? x[c] : 0u;
-                        }
-                        const f32x16_t add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_as_bf16(x), pf, f32x16_t{}, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) o[u][r] += sees ? add[r] : 0.f;
-                    }
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                u32x4_t x = *(const u32x4_t *)values_at(stage, blk, u);
-                if constexpr (!FP8)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if ((x[c] & 0x7F80u) == 0x7F80u) x[c] &= 0xFFFF0000u;
-                        if ((x[c] & 0x7F800000u) == 0x7F800000u) x[c] &= 0xFFFFu;
-                    }
-                o[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kv_as_bf16(x), pf, o[u], 0, 0, 0);
-            }
-        }
+        for (int r = 0; r < 16 * SUBS; ++r) pf[r >> 3][r & 7] = (__bf16)s[r >> 4][r & 15];
     };
 
-    if (stages > 0) {
-        int is_page, next_is_page = 0, over_next_is_page = 0;
-        look_up(first);
-        is_page = fetch(first);
-        look_up(first + KEYS);
-        put(0);
-        if (stages > 1) next_is_page = fetch(first + KEYS);
-        look_up(first + 2 * KEYS);
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
+    for (int i = 0; i < NS; ++i)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) qx[i][c] = valid && q_at(i) < a.pool.dim ? qx[i][c] ^ a.negate : 0u;
-        int buffer = 0, next_buffer = 1;
+        for (int c = 0; c < 4; ++c) qx[i][c] = valid && q_at(i) < a.pool.dim ? qx[i][c] ^ a.negate : 0u;
+    // The sums are changed by the products and by nothing else: were they brought down where a maximum grows, the compiler would move
+    // all of them from registers to registers in every stage.  A maximum that grows too far, to powers that could leave the range, has the
+    // tile done again, with the maxima that are known by then.
 #pragma unroll 1
-        for (int stage = 0; stage < stages; ++stage) {
-            const int at = first + stage * KEYS;
-            if (stage + 1 < stages) {
-                put(next_buffer);
-                if (stage + 2 < stages) over_next_is_page = fetch(at + 2 * KEYS);
-                look_up(at + 3 * KEYS);
+    for (int turn = 0; stages > 0; ++turn) {
+        if (threadIdx.x < 2) found[threadIdx.x] = 0;
+        if (threadIdx.x < 4 * BLOCKS) held[threadIdx.x] = 1;
+        __syncthreads();
+        odd = 0;
+        look_up(0);
+        fetch_keys(0);
+        look_up(1);
+        if (careful) take_care(0);  // (no values yet)
+        put_keys(0);
+        next();
+        fetch_keys(1);
+        fetch_values();
+        next();
+        look_up(2);
+        __syncthreads();
+        if (late) __syncthreads();
+        // what was fetched goes to LDS: keys that the next phase of products reads and values of the one after; the next are asked for
+        auto forward = [&](int i) __attribute__((always_inline)) {
+            put_keys(i + 2);
+            put_values(i + 1);
+            fetch_keys(i + 3);
+            fetch_values();
+            next();
+            look_up(i + 4);
+        };
+        f32x16_t s[SUBS];
+        if (careful) take_care(1);
+        forward(-1);
+        scores(0, s);
+        __syncthreads();
+        weigh(0, s);
+        __syncthreads();
+#pragma unroll 1
+        for (int i = 0; i + 1 < stages; ++i) {
+            if (careful) take_care(i + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            // scores and sums in turn, so that no product waits for the one before it
+            constexpr int PRODUCTS = SUBS * NS + BLOCKS * NU;
+            static_assert(SUBS * NS == BLOCKS * NU, "as many scores as sums");
+            bf16x8_t x[KV_AHEAD];
+            auto operand = [&](int c) __attribute__((always_inline)) {
+                return *(const bf16x8_t *)(c & 1 ? values_at(i, (c >> 1) / NU, (c >> 1) % NU) : keys_at(i + 1, (c >> 1) % SUBS, (c >> 1) / SUBS));
+            };
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub) s[sub] = f32x16_t{};
+#pragma unroll
+            for (int c = 0; c < KV_AHEAD; ++c) x[c] = operand(c);
+#pragma unroll
+            for (int c = 0; c < PRODUCTS; ++c) {
+                const int d = c >> 1;
+                if (c & 1) o[d % NU] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c % KV_AHEAD], pf[d / NU], o[d % NU], 0, 0, 0);
+                else s[d % SUBS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c % KV_AHEAD], kv_as_bf16(qx[d / SUBS]), s[d % SUBS], 0, 0, 0);
+                if (c + KV_AHEAD < PRODUCTS) x[c % KV_AHEAD] = operand(c + KV_AHEAD);
+                __builtin_amdgcn_sched_barrier(KV_MASK);
+                if (c == KV_FORWARD) {
+                    forward(i);
+                    __builtin_amdgcn_sched_barrier(KV_MASK);
+                }
             }
-            __syncthreads();  // this stage is there; nobody is at work on the one before the last any more
-            if (is_page != (1 << BLOCKS) - 1 && threadIdx.x == 0) atomicAdd(a.pool.bad, 1ull);
-            const char *here = lds + buffer * C::STAGE;
-            if (any && at < mine.hi && at + KEYS > mine.lo) {
-                if (at + KEYS > mine.all_hi || at < mine.all_lo || is_page != (1 << BLOCKS) - 1) step_edge(here, at, is_page);
-                else step(here);
+            __syncthreads();
+            weigh(i + 1, s);
+            __syncthreads();
+        }
+        add_values(stages - 1, pf);
+        if (C::NW == 8 && !late) __syncthreads();
+        // Powers beyond 2^32, or sums that left the range with powers above one?
+        bool again = (peak - m) * a.scale > 32.f;
+        if ((peak - m) * a.scale > 0.f) {
+            again = again || !(fabsf(l) <= 3.4e38f);
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) again = again || !(fabsf(o[u][r]) <= 3.4e38f);
+        }
+        if (any && again) found[1] = 1;
+        if (odd & 0x80008000u) found[0] = 1;
+        __syncthreads();
+        const int strange = found[0], once_more = found[1] | strange;
+        __syncthreads();
+        if (turn > 0 || !once_more) break;
+        careful = strange != 0;
+        m = peak;
+        l = 0.f;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) o[u] = f32x16_t{};
+    }
+    if (!FP8 && any && careful) {  // values that were taken out, for the rows that see them: whatever their weight, they decide
+        const int past = first + stages * KEYS, to = mine.hi < past ? mine.hi : past;
+#pragma unroll 1
+        for (int at = mine.lo > first ? mine.lo & ~15 : first; at < to; at += 16) {
+            const int e = kv_page_entry(a.pool, a.batch, t.s.b, at);
+            if (!kv_is_page(a.pool, e)) continue;
+            const bf16_t *block = (const bf16_t *)a.pool.v + kv_block_at(a.pool, e, head, at);
+            bool odd = false;
+            for (int c = lane; c < 2 * DP; c += 64) {
+                const u32x4_t x = *(const u32x4_t *)(block + c * 8);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) odd = odd || kv_not_finite(x[k]);
             }
-            buffer = next_buffer;
-            next_buffer = next_buffer == 2 ? 0 : next_buffer + 1;
-            is_page = next_is_page;
-            next_is_page = over_next_is_page;
+            if (__ballot(odd) == 0) continue;
+#pragma unroll 1
+            for (int key = 0; key < 16; ++key) {
+                const int p = at + key;
+                const bool sees = p <= pos && (a.window == 0 || p > pos - a.window);
+                const bf16_t *v = block + (size_t)kv_half(key) * DP * 8 + kv_slot(key);
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bf16_t x = v[(32 * u + 8 * (r >> 2) + 4 * h + (r & 3)) * 8];
+                        if ((x & 0x7F80u) == 0x7F80u && sees) o[u][r] += bf16_to_f32(x);
+                    }
+            }
         }
     }
     if (!any) return;
@@ -996,7 +1087,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) 
 }
 
 // Workgroups that run at once on 256 compute units.
-static int kv_chunk_workgroups(int dp) { return dp == 64 ? 768 : 256; }
+static int kv_chunk_workgroups(int dp) { return dp == 64 ? 512 : 256; }
 
 template <int DP, bool FP8>
 static int attend_chunks(siso_kv *kv, KvAttend &a, int few) {
@@ -1059,6 +1150,7 @@ extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch
     if (heads < 1 || heads % kv->kv_heads != 0 || heads / kv->kv_heads > 128)
         return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: %d heads over %d kv heads", heads, kv->kv_heads);
     if (!(fabsf(scale) <= 3.0e38f) || window < 0) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: scale %g, window %d", (double)scale, window);
+    if ((long)a.batch.rows * heads > 1L << 30) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: %d rows of %d heads", a.batch.rows, heads);
     if (a.batch.n == 0 || a.batch.rows == 0) return SISO_OK;
     if (!q || !out || ((uintptr_t)q & 1) || ((uintptr_t)out & 15) || ((uintptr_t)lse & 3))
         return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: queries and outputs must be there, outputs 16-byte aligned");
