@@ -20,6 +20,7 @@ struct KvAttend {
     float scale;       // its size times log2(e), above zero: the softmax is one of powers of two
     unsigned negate;   // a scale below zero: the queries' signs are turned
     int window;        // 0 = all
+    int few;           // a sequence of more rows of work is k_kv_attend_chunk's, all others k_kv_attend_few's
     bf16_t *out;
     float *lse;
     float *parts;       // [2 * KV_STRETCHES]: sums [32][DP], then maximum and sum of each row
@@ -107,6 +108,10 @@ __device__ __forceinline__ void kv_finish(const KvAttend &a, const KvTile &t, in
 // are, and nobody but the device knows them.  Tiles and stretches are at most tiles + KV_STRETCHES items, at most 2 * KV_STRETCHES of them
 // parts of a tile that is cut.
 #define KV_FEW 128
+// Of up to 128 elements all sequences go to the one kernel, whatever their rows, where the work is light: its latency is
+// lower, as it has no stages that wait for each other, but every 32 rows read the keys again.  Here tiles times positions times elements; 16
+// heads over 4, 250 rows of 4,000: 27 us for elements of 128 (two kernels: 35), 22 of 64 (26); 400 rows: 44 (39) and 22 (26); 1,000 of 3,000: 40 of 64 (32).
+#define KV_LIGHT (1L << 26)
 #define KV_STRETCHES 1024
 #define KV_LEAST 4  // units of a stretch, at least: one for each wave
 #define KV_ENOUGH 32 // units that are worth being joined
@@ -134,7 +139,7 @@ struct KvFew {
         first = s.first;
         rows = s.rows;
         length = s.length;
-        if (rows == 0 || rows > KV_FEW || rows * a.group > KV_FEW) return;
+        if (rows == 0 || rows * a.group > a.few) return;
         int from;
         tiles = ((rows * a.group + 31) >> 5) * a.pool.kv_heads;
         range = range_of(a, s.start, length, from);
@@ -573,48 +578,78 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAtte
             // few rows leave threads idle: these take every second, fourth or eighth part
             const int work = t.rows * (DP / 4), across = work > 128 ? 1 : work > 64 ? 2 : work > 32 ? 4 : 8, wide = 256 / across;
             const int mine = threadIdx.x & (wide - 1), lead = threadIdx.x / wide;
-            for (int i = mine; i < work || across > 1; i += wide) {
-                const int r = i < work ? i / (DP / 4) : 0, d = i % (DP / 4) * 4;
-                float top = -INFINITY, sum = 0.f;
-                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int s0 = lead; s0 < count; s0 += 8 * across) {
-                    float2 ml[8], y[8], z[8];
+            // ITEMS of a thread's fours of sums at a time, from part `lead` on every `across`th one, PARTS of them on their way at once (what is beyond the last
+            // weighs nothing)
+            auto add_parts = [&](auto items, auto parts_at_once, int i0, float (&top)[decltype(items)::value], float (&sum)[decltype(items)::value],
+                                 float4 (&x)[decltype(items)::value]) __attribute__((always_inline)) {
+                constexpr int ITEMS = decltype(items)::value, PARTS = decltype(parts_at_once)::value;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {  // (all on their way at once; what is beyond the last weighs nothing)
-                        const float *p = part_of(s0 + j * across < count ? s0 + j * across : 0);
-                        ml[j] = kv_found(p + 32 * DP + 2 * r);
-                        y[j] = kv_found(p + r * DP + d);
-                        z[j] = kv_found(p + r * DP + d + 2);
-                    }
-                    float now = top;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (s0 + j * across < count) now = fmaxf(now, ml[j].x);
-                    const float4 had = x;
-                    const float had_sum = sum;
-                    x = make_float4(0.f, 0.f, 0.f, 0.f);
-                    sum = 0.f;
-                    kv_add_part(top, now, had_sum, had, sum, x);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (s0 + j * across < count) kv_add_part(ml[j].x, now, ml[j].y, make_float4(y[j].x, y[j].y, z[j].x, z[j].y), sum, x);
-                    top = now;
+                for (int k = 0; k < ITEMS; ++k) {
+                    top[k] = -INFINITY;
+                    sum[k] = 0.f;
+                    x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
                 }
-                if (across > 1) {
-                    *(float4 *)(sh + 8 * threadIdx.x) = x;
-                    *(float2 *)(sh + 8 * threadIdx.x + 4) = make_float2(top, sum);
-                    __syncthreads();
-                    if (lead != 0 || i >= work) break;
-                    for (int j = 1; j < across; ++j) top = fmaxf(top, sh[8 * (j * wide + mine) + 4]);
-                    x = make_float4(0.f, 0.f, 0.f, 0.f);
-                    sum = 0.f;
+                for (int s0 = lead; s0 < count; s0 += PARTS * across) {
+                    float2 ml[ITEMS][PARTS], y[ITEMS][PARTS], z[ITEMS][PARTS];
+#pragma unroll
+                    for (int k = 0; k < ITEMS; ++k) {
+                        const int i = i0 + k * wide < work ? i0 + k * wide : 0, r = i / (DP / 4), d = i % (DP / 4) * 4;
+#pragma unroll
+                        for (int j = 0; j < PARTS; ++j) {
+                            const float *p = part_of(s0 + j * across < count ? s0 + j * across : 0);
+                            ml[k][j] = kv_found(p + 32 * DP + 2 * r);
+                            y[k][j] = kv_found(p + r * DP + d);
+                            z[k][j] = kv_found(p + r * DP + d + 2);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < ITEMS; ++k) {
+                        float now = top[k];
+#pragma unroll
+                        for (int j = 0; j < PARTS; ++j)
+                            if (s0 + j * across < count) now = fmaxf(now, ml[k][j].x);
+                        const float4 had = x[k];
+                        const float had_sum = sum[k];
+                        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        sum[k] = 0.f;
+                        kv_add_part(top[k], now, had_sum, had, sum[k], x[k]);
+#pragma unroll
+                        for (int j = 0; j < PARTS; ++j)
+                            if (s0 + j * across < count)
+                                kv_add_part(ml[k][j].x, now, ml[k][j].y, make_float4(y[k][j].x, y[k][j].y, z[k][j].x, z[k][j].y), sum[k], x[k]);
+                        top[k] = now;
+                    }
+                }
+            };
+            if (across == 1) {
+                constexpr int ITEMS = 2;
+                for (int i0 = mine; i0 < work; i0 += ITEMS * wide) {
+                    float top[ITEMS], sum[ITEMS];
+                    float4 x[ITEMS];
+                    add_parts(std::integral_constant<int, ITEMS>(), std::integral_constant<int, 5>(), i0, top, sum, x);
+#pragma unroll
+                    for (int k = 0; k < ITEMS; ++k) {
+                        const int i = i0 + k * wide;
+                        if (i < work) kv_finish(a, t, head, i / (DP / 4), i % (DP / 4) * 4, top[k], sum[k], x[k]);
+                    }
+                }
+            } else {
+                float top[1], sum[1];
+                float4 x[1];
+                add_parts(std::integral_constant<int, 1>(), std::integral_constant<int, 8>(), mine, top, sum, x);
+                *(float4 *)(sh + 8 * threadIdx.x) = x[0];
+                *(float2 *)(sh + 8 * threadIdx.x + 4) = make_float2(top[0], sum[0]);
+                __syncthreads();
+                if (lead == 0 && mine < work) {
+                    for (int j = 1; j < across; ++j) top[0] = fmaxf(top[0], sh[8 * (j * wide + mine) + 4]);
+                    x[0] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    sum[0] = 0.f;
                     for (int j = 0; j < across; ++j) {
                         const float *other = sh + 8 * (j * wide + mine);
-                        kv_add_part(other[4], top, other[5], *(const float4 *)other, sum, x);
+                        kv_add_part(other[4], top[0], other[5], *(const float4 *)other, sum[0], x[0]);
                     }
+                    kv_finish(a, t, head, mine / (DP / 4), mine % (DP / 4) * 4, top[0], sum[0], x[0]);
                 }
-                kv_finish(a, t, head, r, d, top, sum, x);
-                if (across > 1) break;
             }
         }
     }
@@ -650,7 +685,6 @@ struct KvChunk {
 struct KvPieces {
     long slots, slot0;
     int ways;  // a tile's positions are cut into at most so many pieces
-    int few;   // sequences of at most so many rows of work are left to k_kv_attend_few
 };
 #define KV_PIECE_LEAST 256  // positions
 // A phase of products: operands are read so many products ahead (4: 1% slower, 8: 2%), and the work of the next stages begins behind this one.
@@ -667,7 +701,7 @@ __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces 
     const int b = kv_sequence_of(a.batch, slot, a.group, SHIFT, 1);
     t.s = kv_sequence(a.batch, b);
     const long j = slot - kv_slots_before(t.s.first, b, a.group, SHIFT, 1), work = (long)t.s.rows * a.group;
-    if (j < 0 || j * ROWS >= work || work <= p.few) return false;
+    if (j < 0 || j * ROWS >= work || work <= a.few) return false;
     kv_tile(a, (int)(j * ROWS), ROWS, t);
     from = t.lo & ~(KEYS - 1);
     blocks = t.hi > from ? (t.hi - from + KEYS - 1) / KEYS : 0;
@@ -1060,7 +1094,7 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
     if (valid && h == 0 && a.lse) a.lse[at_out] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f;
 }
 
-// Joins the pieces of the tiles that were cut, in their order: eight workgroups for a tile.
+// Joins the pieces of the tiles that were cut, in their order, four elements a thread.
 template <int DP, bool FP8>
 __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) {
     using C = KvChunk<DP, FP8>;
@@ -1071,13 +1105,14 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) 
     if (!kv_chunk_tile<C::ROWS, C::KEYS>(a, p, p.slot0 + p.slots - 1 - at_slot, t, from, blocks, per, pieces) || pieces <= 1) return;
     const float *parts = a.parts + (size_t)(at_slot * p.ways * a.pool.kv_heads + head) * KV_CHUNK_PART(C::ROWS, DP);
     const size_t next = (size_t)a.pool.kv_heads * KV_CHUNK_PART(C::ROWS, DP);
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < t.rows * (DP / 4); i += 256 * gridDim.y) {
+    const int i = blockIdx.y * 256 + threadIdx.x;
+    if (i < t.rows * (DP / 4)) {
         const int r = i / (DP / 4), d = i % (DP / 4) * 4;
         float top = -INFINITY, sum = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
         for (int s = 0; s < pieces; ++s) top = fmaxf(top, parts[s * next + C::ROWS * DP + 2 * r]);
-#pragma unroll 4
+#pragma unroll 8
         for (int s = 0; s < pieces; ++s) {
             const float2 ml = *(const float2 *)(parts + s * next + C::ROWS * DP + 2 * r);
             kv_add_part(ml.x, top, ml.y, *(const float4 *)(parts + s * next + r * DP + d), sum, x);
@@ -1090,10 +1125,9 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) 
 static int kv_chunk_workgroups(int dp) { return dp == 64 ? 512 : 256; }
 
 template <int DP, bool FP8>
-static int attend_chunks(siso_kv *kv, KvAttend &a, int few) {
+static int attend_chunks(siso_kv *kv, const KvAttend &a) {
     using C = KvChunk<DP, FP8>;
     KvPieces p;
-    p.few = few;
     p.slots = kv_slots_before(a.batch.rows, a.batch.n, a.group, C::ROWS == 256 ? 8 : 7, 1);
     const long tiles = p.slots * kv->kv_heads, room = (long)(SISO_KV_PARTS / KV_CHUNK_PART(C::ROWS, DP));
     long ways = tiles <= kv_chunk_workgroups(DP) / 2 ? kv_chunk_workgroups(DP) / tiles : 1;
@@ -1108,7 +1142,7 @@ static int attend_chunks(siso_kv *kv, KvAttend &a, int few) {
         hipLaunchKernelGGL((k_kv_attend_chunk<DP, FP8>), dim3((unsigned)(p.slots * ways * kv->kv_heads)), dim3(C::NT), C::LDS, kv->stream, a, p);
         KV_TRY(kv, hipGetLastError());
         if (ways > 1) {
-            hipLaunchKernelGGL((k_kv_attend_join<DP, FP8>), dim3((unsigned)(p.slots * kv->kv_heads), 8), dim3(256), 0, kv->stream, a, p);
+            hipLaunchKernelGGL((k_kv_attend_join<DP, FP8>), dim3((unsigned)(p.slots * kv->kv_heads), C::ROWS * (DP / 4) / 256), dim3(256), 0, kv->stream, a, p);
             KV_TRY(kv, hipGetLastError());
         }
     }
@@ -1118,8 +1152,11 @@ static int attend_chunks(siso_kv *kv, KvAttend &a, int few) {
 template <int DP, bool FP8>
 static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
     // Which sequences there are is known on the device only: where both kinds can be, both kernels are launched, and each leaves the other's.
-    if (max_new * a.group > KV_FEW) {
-        const int rc = attend_chunks<DP, FP8>(kv, a, KV_FEW);
+    const long seen = a.window > 0 && a.window + 32L < max_length ? a.window + 32L : max_length;
+    const long light = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads * seen;
+    a.few = DP <= 128 && light * DP <= KV_LIGHT ? 1 << 30 : KV_FEW;
+    if (max_new * a.group > a.few) {
+        const int rc = attend_chunks<DP, FP8>(kv, a);
         if (rc != SISO_OK || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
     }
     constexpr int KS = kv_step(DP);

@@ -16,7 +16,10 @@ struct KvVerify {
     long item0;
 };
 #define KV_SLICES 256  // of a row, at most: one for each thread of the workgroup that joins them
-#define KV_FILL 2048 // workgroups
+// Workgroups.  Drawing: as many as are on the chip at once (64 rows of 128,001 with a draft's: 22.2 us; 2,048 come in two turns, 25.5 us; 512: 24.5).
+// Greedy: 2,048 (250 rows of 65,537 in 16 bits 15.4 us; 1,024: 21.2).
+#define KV_FILL_DRAW 1024
+#define KV_FILL 2048
 #define KV_SLICE_UNIT 2048  // 256 threads, eight entries each
 
 // Eight entries from e on of a row that begins anywhere (a row of an odd vocabulary is aligned to its type only).
@@ -373,7 +376,7 @@ extern "C" int siso_kv_verify(siso_kv *kv, const siso_kv_batch *batch, const int
     // as many slices as fill the chip, of one unit at least (a part of each fits the workspace: KV_FILL of them, or one for each row)
     const long units = (vocab + KV_SLICE_UNIT - 1) / KV_SLICE_UNIT, rows = a.batch.rows > 0 ? a.batch.rows : 1;
     const long max_new = batch->max_new > 0 && batch->max_new < rows ? batch->max_new : rows;
-    long slices = KV_FILL / (u_accept ? a.batch.n : rows);
+    long slices = u_accept ? KV_FILL_DRAW / a.batch.n : KV_FILL / rows;
     slices = slices > KV_SLICES ? KV_SLICES : slices;
     slices = slices < 1 ? 1 : slices > units ? units : slices;
     a.slice = (int)((units + slices - 1) / slices * KV_SLICE_UNIT);
