@@ -109,9 +109,14 @@ __device__ __forceinline__ void kv_finish(const KvAttend &a, const KvTile &t, in
 // parts of a tile that is cut.
 #define KV_FEW 128
 // Of up to 128 elements all sequences go to the one kernel, whatever their rows, where the work is light: its latency is
-// lower, as it has no stages that wait for each other, but every 32 rows read the keys again.  Here tiles times positions times elements; 16
-// heads over 4, 250 rows of 4,000: 27 us for elements of 128 (two kernels: 35), 22 of 64 (26); 400 rows: 44 (39) and 22 (26); 1,000 of 3,000: 40 of 64 (32).
+// lower, as it has no stages that wait for each other, but every 32 rows read the keys again.  Light are so many tiles times positions times
+// elements at most, all taken to be as long as the longest: KV_LIGHT where all sequences have as many new rows (16 heads over 4, 250 rows of
+// 4,000: 25 us for elements of 128, two kernels 35; of 64 21 and 26; 400 rows: 41 and 39, 21 and 26; 1,000 rows of 3,000: 60 and 46, 38 and
+// 32), KV_LIGHT_MIXED where not: then both kernels would run, one after the other, and this one's stretches are alike however lengths
+// differ (8 heads, 24 sequences of 1 to 1,500 rows and 1 to 5,000 positions, elements of 128: 80 us, two kernels 128;
+// 32 heads, 64 sequences of up to 4,000 rows and 9,000 positions: 1,377 and 1,007).
 #define KV_LIGHT (1L << 26)
+#define KV_LIGHT_MIXED (1L << 30)
 #define KV_STRETCHES 1024
 #define KV_LEAST 4  // units of a stretch, at least: one for each wave
 #define KV_ENOUGH 32 // units that are worth being joined
@@ -1154,7 +1159,7 @@ static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
     // Which sequences there are is known on the device only: where both kinds can be, both kernels are launched, and each leaves the other's.
     const long seen = a.window > 0 && a.window + 32L < max_length ? a.window + 32L : max_length;
     const long light = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads * seen;
-    a.few = DP <= 128 && light * DP <= KV_LIGHT ? 1 << 30 : KV_FEW;
+    a.few = DP <= 128 && light * DP <= (a.batch.rows >= max_new * a.batch.n ? KV_LIGHT : KV_LIGHT_MIXED) ? 1 << 30 : KV_FEW;
     if (max_new * a.group > a.few) {
         const int rc = attend_chunks<DP, FP8>(kv, a);
         if (rc != SISO_OK || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
