@@ -268,6 +268,8 @@ __device__ __forceinline__ void kv_turn_back(const u32x4_t (&in)[4], uint2 (&out
 __device__ __forceinline__ int kv_token(int half, int s) { return (s & 3) + 4 * half + 8 * (s >> 2); }  // of a half's eight
 __device__ __forceinline__ size_t kv_v8_at(int dp, int h, int d) { return (((h * (dp >> 6) + (d >> 6)) * 32 + (d & 31)) * 2 + ((d >> 5) & 1)) * 8; }
 
+// Bound by bytes where there are many rows: 21,692 rows of 8 heads of 128 into 8 bits, 135 MB, in 33 us, 4.1 TB/s.  Few rows (8: 5 us, an empty launch
+// takes half of that) wait for sequence, page and row, one after the other: a block is 16 tokens so that there are many to wait at a time.
 // NC: chunks of 8 elements per thread (dp <= 128: one, else two)
 template <int NC, bool FP8>
 __global__ __launch_bounds__(256) void k_kv_write(KvPool pool, KvBatch batch, const bf16_t *k, long k_token, long k_head, const bf16_t *v,
@@ -376,6 +378,7 @@ __device__ __forceinline__ void kv_decode8(uint2 codes, float scale, float (&x)[
     }
 }
 
+// The other way round; the same rows into 16 bits in 25 us, 5.4 TB/s.
 template <int NC, bool FP8, class O>
 __global__ __launch_bounds__(256) void k_kv_read(KvPool pool, KvBatch batch, O *out_k, O *out_v, long slot0) {
     constexpr int DP = NC * 128;
