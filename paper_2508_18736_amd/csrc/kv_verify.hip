@@ -16,10 +16,12 @@ struct KvVerify {
     long item0;
 };
 #define KV_SLICES 256  // of a row, at most: one for each thread of the workgroup that joins them
-// Workgroups.  Drawing: as many as are on the chip at once (64 rows of 128,001 with a draft's: 22.2 us; 2,048 come in two turns, 25.5 us; 512: 24.5).
-// Greedy: 2,048 (250 rows of 65,537 in 16 bits 15.4 us; 1,024: 21.2).
-#define KV_FILL_DRAW 1024
-#define KV_FILL 2048
+// Workgroups.  Drawing: as many as are on the chip at once (64 rows of 128,001 with a draft's: 22.2 us; 2,048 come in two turns, 25.5 us; 512:
+// 24.5).  Greedy, 64 sequences of 1 to 5 rows of 50,000: 13.5 us, 2,048 17.0; of 5 to 9 rows of 130,000 in 16 bits 38.5 and 31.3.
+#define KV_FILL 1024
+// Workgroups of a sequence, greedy: they count themselves at one address, one after the other (8 sequences of 1 to 9 rows of 128,000: 11.7 us; 128:
+// 14.0, as many as there are slices and rows: 21.5).
+#define KV_ARRIVE 64
 #define KV_SLICE_UNIT 2048  // 256 threads, eight entries each
 
 // Eight entries from e on of a row that begins anywhere (a row of an odd vocabulary is aligned to its type only).
@@ -320,21 +322,28 @@ __global__ __launch_bounds__(256) void k_kv_follow(KvVerify a) {
     }
     if (!kv_last(a.arrived + b, (unsigned)(s.rows < a.lanes ? s.rows : a.lanes) * a.slices)) return;
 
+    __shared__ u64 largest[64];
     int accepted = 0, following = -1;
-    for (int i0 = 0; i0 < s.rows; i0 += 64) {  // (every wave by itself)
-        const int i = i0 + (t & 63);
+    for (int i0 = 0; i0 < s.rows; i0 += 64) {
+        // all parts of 64 rows, side by side in memory, a thread for each
+        const int here = s.rows - i0 < 64 ? s.rows - i0 : 64, parts = here * a.slices;
+        const u64 *of_rows = a.parts + (long)(s.first + i0) * a.slices;
+        if (t < 64) largest[t] = 0;
+        __syncthreads();
+        for (int j0 = t; j0 < parts; j0 += 4 * 256) {
+            u64 k[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) k[c] = kv_part(of_rows + (j0 + 256 * c < parts ? j0 + 256 * c : j0));
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (j0 + 256 * c < parts) atomicMax((unsigned long long *)&largest[(j0 + 256 * c) / a.slices], (unsigned long long)k[c]);
+        }
+        __syncthreads();
+        const int i = i0 + (t & 63);  // (every wave by itself)
         int best = -1;
         bool good = false;
         if (i < s.rows) {
-            u64 most = 0;
-            const u64 *of_row = a.parts + (long)(s.first + i) * a.slices;
-            for (int j = 0; j < a.slices; j += 8) {
-                u64 k[8];
-#pragma unroll
-                for (int c = 0; c < 8; ++c) k[c] = kv_part(of_row + (j + c < a.slices ? j + c : j));
-#pragma unroll
-                for (int c = 0; c < 8; ++c) most = k[c] > most ? k[c] : most;
-            }
+            const u64 most = largest[t & 63];
             if (most != 0) best = (int)(0xFFFFFFFFu - (unsigned)most);
             good = i < s.rows - 1 && best >= 0 && best == a.tokens[s.first + i + 1];
         }
@@ -342,7 +351,8 @@ __global__ __launch_bounds__(256) void k_kv_follow(KvVerify a) {
         const int stop = refused ? __ffsll((long long)refused) - 1 : 64;
         accepted = i0 + stop;
         following = __shfl(best, stop & 63);
-        if (stop < 64) break;  // (the last row is never `good`: this ends at the latest there)
+        if (stop < 64) break;  // (the last row is never `good`: this ends at the latest there; the same in every wave)
+        __syncthreads();
     }
     kv_write_tokens(a, s, accepted, following);
 }
@@ -376,20 +386,23 @@ extern "C" int siso_kv_verify(siso_kv *kv, const siso_kv_batch *batch, const int
     a.parts = (u64 *)kv->parts;
     a.arrived = kv->arrived;
     a.item0 = 0;
-    // as many slices as fill the chip, of one unit at least (a part of each fits the workspace: KV_FILL of them, or one for each row)
+    // as many slices as fill the chip, of one unit at least (greedy: a part of each for each row; the workspace has room for one of 2^24)
     const long units = (vocab + KV_SLICE_UNIT - 1) / KV_SLICE_UNIT, rows = a.batch.rows > 0 ? a.batch.rows : 1;
     const long max_new = batch->max_new > 0 && batch->max_new < rows ? batch->max_new : rows;
-    long slices = u_accept ? KV_FILL_DRAW / a.batch.n : KV_FILL / rows;
+    long lanes = 1, slices;
+    if (u_accept) slices = KV_FILL / a.batch.n;
+    else {  // four rows keep a workgroup busy
+        lanes = KV_FILL / a.batch.n < (max_new + 3) / 4 ? KV_FILL / a.batch.n : (max_new + 3) / 4;
+        lanes = lanes < 1 ? 1 : lanes;
+        slices = KV_FILL / (a.batch.n * lanes);
+        slices = slices * lanes > KV_ARRIVE ? KV_ARRIVE / lanes : slices;
+        slices = slices * rows > (long)(SISO_KV_PARTS / 2) ? (long)(SISO_KV_PARTS / 2) / rows : slices;
+    }
     slices = slices > KV_SLICES ? KV_SLICES : slices;
     slices = slices < 1 ? 1 : slices > units ? units : slices;
     a.slice = (int)((units + slices - 1) / slices * KV_SLICE_UNIT);
     a.slices = (vocab + a.slice - 1) / a.slice;
-    a.lanes = 1;
-    if (!u_accept) {  // four rows keep a workgroup busy
-        long lanes = KV_FILL / ((long)a.batch.n * a.slices);
-        lanes = lanes > (max_new + 3) / 4 ? (max_new + 3) / 4 : lanes;
-        a.lanes = lanes < 1 ? 1 : (int)lanes;
-    }
+    a.lanes = (int)lanes;
     const long all = (long)a.batch.n * a.slices * a.lanes, piece = 1L << 23;
     for (; a.item0 < all; a.item0 += piece) {  // (a launch has fewer than 2^32 threads)
         const dim3 grid((unsigned)(all - a.item0 < piece ? all - a.item0 : piece));
