@@ -144,7 +144,13 @@ extern "C" long siso_kv_bad_pages(siso_kv *kv) {
 struct KvBlock {
     KvSequence s;
     int at;    // position of the block's first token
-    int page;  // -1: none
+    int page;  // what the table says of it
+    // Is that a page?  Asked after what does not depend on it has been sent for.
+    __device__ __forceinline__ bool held(const KvPool &pool) const {
+        const bool is = kv_is_page(pool, page);
+        if (!is && threadIdx.x == 0) atomicAdd(pool.bad, 1ull);
+        return is;
+    }
 };
 
 // Slots for siso_kv_write and siso_kv_read: m rows stand in at most m / 16 + 2 blocks.
@@ -155,14 +161,12 @@ static long kv_block_slots(const KvBatch &b) {
 }
 
 __device__ __forceinline__ bool kv_find_block(const KvPool &pool, const KvBatch &batch, long slot, KvBlock &k) {
-    const int b = batch.single ? (int)slot : kv_sequence_of(batch, slot, 1, KV_BLOCK_SHIFT, KV_BLOCK_EXTRA);
-    k.s = kv_sequence(batch, b);
-    const long j = batch.single ? 0 : slot - kv_slots_before(k.s.first, b, 1, KV_BLOCK_SHIFT, KV_BLOCK_EXTRA);
+    k.s = batch.single ? kv_sequence(batch, (int)slot) : kv_sequence_of(batch, slot, 1, KV_BLOCK_SHIFT, KV_BLOCK_EXTRA);
+    const long j = batch.single ? 0 : slot - kv_slots_before(k.s.first, k.s.b, 1, KV_BLOCK_SHIFT, KV_BLOCK_EXTRA);
     const long at = (long)((k.s.start > 0 ? k.s.start : 0) >> 4) * SISO_KV_BLOCK + j * SISO_KV_BLOCK;
     if (j < 0 || at >= k.s.length || k.s.rows == 0) return false;
     k.at = (int)at;
-    k.page = kv_page(pool, batch, b, k.at);
-    if (k.page < 0 && threadIdx.x == 0) atomicAdd(pool.bad, 1ull);
+    k.page = kv_page_entry(pool, batch, k.s.b, k.at);
     return true;
 }
 
@@ -279,7 +283,7 @@ __global__ __launch_bounds__(256) void k_kv_write(KvPool pool, KvBatch batch, co
     __shared__ __attribute__((aligned(16))) char turn[SISO_KV_BLOCK * (DP + 8) * ES];
     const int head = blockIdx.x % pool.kv_heads;
     KvBlock blk;
-    if (!kv_find_block(pool, batch, slot0 + blockIdx.x / pool.kv_heads, blk) || blk.page < 0) return;
+    if (!kv_find_block(pool, batch, slot0 + blockIdx.x / pool.kv_heads, blk)) return;
     const int t = threadIdx.x, key = t >> 4, i = t & 15, dim = pool.dim, dp = pool.dp;
     const int row = blk.at + key - blk.s.start;  // (not below: the first block may begin before the first row)
     const bool in = row >= 0 && row < blk.s.rows;
@@ -292,6 +296,7 @@ __global__ __launch_bounds__(256) void k_kv_write(KvPool pool, KvBatch batch, co
         kx[c] = take ? kv_load8(k + r * k_token + head * k_head + e, vec & 1) : u32x4_t{0, 0, 0, 0};
         vx[c] = take ? kv_load8(v + r * v_token + head * v_head + e, vec & 2) : u32x4_t{0, 0, 0, 0};
     }
+    if (!blk.held(pool)) return;
     char *kb = pool.k + kv_block_at(pool, blk.page, head, blk.at) * ES;
     char *vb = pool.v + kv_block_at(pool, blk.page, head, blk.at) * ES;
     if constexpr (FP8) {
@@ -408,7 +413,7 @@ __global__ __launch_bounds__(256) void k_kv_read(KvPool pool, KvBatch batch, O *
     if (!some) return;
     const int row = blk.at + key - blk.s.start;
     const bool in = row >= 0 && row < blk.s.rows;
-    const bool held = blk.page >= 0;
+    const bool held = blk.held(pool);
     const int page = held ? blk.page : 0;
     using K = typename std::conditional<FP8, uint2, u32x4_t>::type;       // eight elements
     using Four = typename std::conditional<FP8, unsigned, uint2>::type;  // four

@@ -707,9 +707,8 @@ template <int ROWS, int KEYS>
 __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces &p, long slot, KvTile &t, int &from, int &blocks, int &per, int &pieces) {
     constexpr int SHIFT = ROWS == 256 ? 8 : 7;
     static_assert(ROWS == 1 << SHIFT, "rows of a tile");
-    const int b = kv_sequence_of(a.batch, slot, a.group, SHIFT, 1);
-    t.s = kv_sequence(a.batch, b);
-    const long j = slot - kv_slots_before(t.s.first, b, a.group, SHIFT, 1), work = (long)t.s.rows * a.group;
+    t.s = kv_sequence_of(a.batch, slot, a.group, SHIFT, 1);
+    const long j = slot - kv_slots_before(t.s.first, t.s.b, a.group, SHIFT, 1), work = (long)t.s.rows * a.group;
     if (j < 0 || j * ROWS >= work || work <= a.few) return false;
     kv_tile(a, (int)(j * ROWS), ROWS, t);
     from = t.lo & ~(KEYS - 1);

@@ -60,18 +60,30 @@ __device__ __forceinline__ KvSequence kv_sequence(const KvBatch &batch, int b) {
     return s;
 }
 
-// The sequence that `slot` belongs to, the same in every lane: the wave looks at 64 sequences at a time.
-__device__ __forceinline__ int kv_sequence_of(const KvBatch &batch, long slot, int group, int shift, int extra) {
+// The sequence that `slot` belongs to, the same in every lane: the wave looks at 64 sequences at a time.  Of up to 64 the lanes already have
+// what is to be known of the one that it is: one wait for memory, not two.
+__device__ __forceinline__ KvSequence kv_sequence_of(const KvBatch &batch, long slot, int group, int shift, int extra) {
     const int lane = threadIdx.x & 63;
+    if (batch.n <= 64) {
+        KvSequence s = kv_sequence(batch, lane < batch.n ? lane : batch.n - 1);
+        const int before = __popcll(__ballot(lane < batch.n && kv_slots_before(s.first, lane, group, shift, extra) <= slot));
+        const int at = before > 0 ? before - 1 : 0;  // (not decreasing: those before come first)
+        s.b = at;
+        s.first = __builtin_amdgcn_readlane(s.first, at);
+        s.rows = __builtin_amdgcn_readlane(s.rows, at);
+        s.length = __builtin_amdgcn_readlane(s.length, at);
+        s.start = s.length - s.rows;
+        return s;
+    }
     int lo = 0, count = batch.n;
     while (count > 1) {
         const int step = (count + 63) / 64, at = lo + lane * step;
         const bool before = lane * step < count && kv_slots_before(kv_clamp(batch.first[at], 0, batch.rows), at, group, shift, extra) <= slot;
-        const int k = __popcll(__ballot(before));  // (not decreasing: those before come first)
+        const int k = __popcll(__ballot(before));
         lo += (k > 0 ? k - 1 : 0) * step;
         count = batch.n - lo < step ? batch.n - lo : step;
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    return kv_sequence(batch, __builtin_amdgcn_readfirstlane(lo));
 }
 
 // What the table says of position `at` (below most, the same in every lane): by a load of the scalar unit, which no vector load
@@ -80,10 +92,6 @@ __device__ __forceinline__ int kv_page_entry(const KvPool &pool, const KvBatch &
     return *(const __attribute__((address_space(4))) int *)(batch.pages + ((long)b * batch.width + (at >> pool.shift)));
 }
 __device__ __forceinline__ bool kv_is_page(const KvPool &pool, int page) { return (unsigned)page < (unsigned)pool.pages; }
-__device__ __forceinline__ int kv_page(const KvPool &pool, const KvBatch &batch, int b, int at) {  // -1: none
-    const int page = kv_page_entry(pool, batch, b, at);
-    return kv_is_page(pool, page) ? page : -1;
-}
 // Where the block of position `at` of a kv head begins, in bytes for elements of one byte (16 bits: twice that).
 __device__ __forceinline__ size_t kv_block_at(const KvPool &pool, int page, int head, int at) {
     return ((size_t)((long)page * pool.kv_heads + head) << pool.shift) * pool.dp + (size_t)(((at & ((1 << pool.shift) - 1)) >> 4) * SISO_KV_BLOCK) * pool.dp;
