@@ -236,11 +236,15 @@ __global__ __launch_bounds__(1024) void k_kv_plan(KvAttend a) {
 // Bound by the reading of keys and values: 64 sequences of one token over 282,144 positions, 32 heads over 8 of 128 in 8 bits, 597 MB, in 120 us, 5.0
 // TB/s (a large copy on the same card: 5.0), two over 232,244 in 16 bits, 951 MB, in 177 us, 5.4 TB/s.  Short ones are bound by latency: one
 // token over 2,001 positions takes 10 us, of which the join is about 3.
-constexpr int kv_step(int dp) { return dp <= 64 ? 64 : 32; }
+// Up to 64 elements a step of 64 positions, where two waves on a SIMD unit have to have enough on their way (24 sequences of up to 12 rows and 30,000
+// positions, 16 bits: 36 us; steps of 32 and three waves 40, four 48), but of codes, which are half the bytes, 32 and four waves (the
+// same 25 and 25 us; 5,261 rows of 40 sequences under a window of 1,000, 12 heads: 49 and 38).
 template <int DP, bool FP8>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAttend a) {
+constexpr int kv_step() { return DP <= 64 && !FP8 ? 64 : 32; }
+template <int DP, bool FP8>
+__global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAttend a) {
     constexpr int ES = FP8 ? 1 : 2;
-    constexpr int KS = kv_step(DP), SUBS = KS / 32, BLOCKS = KS / 16;
+    constexpr int KS = kv_step<DP, FP8>(), SUBS = KS / 32, BLOCKS = KS / 16;
     constexpr int NF = FP8 ? DP / 32 : DP / 16;  // 16-byte operands of a lane for 32 keys, and for 32 values
     constexpr int NU = DP / 32;
     constexpr int RS = DP + 4;  // floats of a row in LDS
@@ -1167,7 +1171,7 @@ static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
         const int rc = attend_chunks<DP, FP8>(kv, a);
         if (rc != SISO_OK || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
     }
-    constexpr int KS = kv_step(DP);
+    constexpr int KS = kv_step<DP, FP8>();
     const long tiles = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads, cuts = (max_length / KS + 2 + KV_LEAST - 1) / KV_LEAST;
     const long items = tiles * cuts < tiles + KV_STRETCHES ? tiles * cuts : tiles + KV_STRETCHES, piece = 1L << 23;
     a.items = items;
