@@ -689,7 +689,7 @@ struct KvChunk {
     static constexpr int NL = (CHUNKS + NT - 1) / NT;      // of a thread
     static constexpr int HALF = KEYS * DP * 2;             // bytes of a stage's keys in LDS
     static constexpr int SCALES = 4 * HALF;                // (8 bits) where the scales begin: of four stages, keys' and values'
-    static constexpr int FOUND = SCALES + (FP8 ? 4 * 2 * KEYS * 4 : 0);  // two words: a value that is not finite, a maximum that grew too far
+    static constexpr int FOUND = SCALES + (FP8 ? 4 * 2 * KEYS * 4 : 0);  // three words: a value that is not finite, a maximum that grew too far, a page that is none
     static constexpr int LDS = FOUND + 16 + 4 * BLOCKS * 4;  // and which blocks of four stages have a page
     static_assert(LDS <= 160 * 1024 && NT >= 2 * KEYS, "fits LDS; a thread for each scale");
 };
@@ -798,7 +798,7 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
             const int c = threadIdx.x + C::NT * i, at = position(stage, c / C::BLOCK_CHUNKS % BLOCKS);
             const bool held = kv_is_page(a.pool, entry[i]);
             k_held = (k_held & ~(1u << i)) | (unsigned)held << i;
-            odd |= held ? 0u : 0x8000u;
+            odd |= held ? 0u : 1u;
             const long off = (held ? entry[i] : 0) * page_bytes + head_bytes + ((at & in_page) >> 4) * (C::BLOCK_CHUNKS * 16) + c % C::BLOCK_CHUNKS * 16;
             gk[i] = *(const u32x4_t *)(a.pool.k + off);
             k_at[i] = a.pool.v + off;
@@ -953,10 +953,11 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
         for (int c = 0; c < 4; ++c) qx[i][c] = valid && q_at(i) < a.pool.dim ? qx[i][c] ^ a.negate : 0u;
     // The sums are changed by the products and by nothing else: were they brought down where a maximum grows, the compiler would move
     // all of them from registers to registers in every stage.  A maximum that grows too far, to powers that could leave the range, has the
-    // tile done again, with the maxima that are known by then.
+    // tile done again, with the maxima that are known by then.  Pages that are none are read as the first page in the first
+    // turn: its maxima do not count then, the careful turn begins without any, and there may be a third.
 #pragma unroll 1
     for (int turn = 0; stages > 0; ++turn) {
-        if (threadIdx.x < 2) found[threadIdx.x] = 0;
+        if (threadIdx.x < 3) found[threadIdx.x] = 0;
         if (threadIdx.x < 4 * BLOCKS) held[threadIdx.x] = 1;
         __syncthreads();
         odd = 0;
@@ -1032,11 +1033,13 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
         }
         if (any && again) found[1] = 1;
         if (odd & 0x80008000u) found[0] = 1;
+        if (odd & 1u) found[2] = 1;
         __syncthreads();
-        const int strange = found[0], once_more = found[1] | strange;
+        const int grown = found[1], no_page = found[2], strange = found[0] | no_page;
         __syncthreads();
-        if (turn > 0 || !once_more) break;
+        if (turn == 0 ? !(grown | strange) : turn > 1 || !(grown & no_page)) break;
         careful = strange != 0;
+        if (turn == 0 && no_page) peak = -INFINITY;
         m = peak;
         l = 0.f;
 #pragma unroll
