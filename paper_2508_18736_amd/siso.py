@@ -568,6 +568,8 @@ class PagedKV:
                              f"tensor on {self.device}")
         if t.stride(2) == 1:
             return t
+        if self._elsewhere():
+            self._used(t)  # (the copy reads it on the handle's stream)
         with torch.cuda.stream(self._stream):  # (a copy is ordered like the call)
             return t.contiguous()
 
