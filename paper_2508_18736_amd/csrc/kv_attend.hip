@@ -151,14 +151,15 @@ struct KvFew {
     }
     __device__ __forceinline__ u64 units() const { return (u64)tiles * (unsigned)range; }
     // Units of a stretch, from how many there are of units and tiles: KV_ENOUGH of them at least, less only where that would not
-    // fill the chip, and so many that there are no more than KV_STRETCHES, nor than the launch has workgroups for.
+    // fill the chip, and so many that there are no more than KV_STRETCHES, nor than the launch has workgroups for.  More tiles than the launch
+    // counted (first rows that decrease) are not cut: a part that no workgroup comes for would leave its tile's count for the next call.
     __device__ __forceinline__ static unsigned stretch_of(const KvAttend &a, u64 all, u64 all_tiles) {
+        if (all_tiles >= (u64)a.items) return 0x7FFFFFFFu;
         const u64 room = a.items - all_tiles < KV_STRETCHES ? a.items - all_tiles : KV_STRETCHES;
-        if (room == 0) return 0x7FFFFFFFu;
         unsigned s = all < KV_FULL * KV_ENOUGH ? (unsigned)all / KV_FULL : KV_ENOUGH;
         s = s > KV_LEAST ? s : KV_LEAST;
-        const unsigned most = (unsigned)((all + room - 1) / room);
-        return s > most ? s : most;
+        const u64 most = (all + room - 1) / room;
+        return most > 0x7FFFFFFFu ? 0x7FFFFFFFu : s > most ? s : (unsigned)most;
     }
     __device__ __forceinline__ unsigned cuts(unsigned stretch) const { return tiles ? ((unsigned)range + stretch - 1) / stretch : 0; }
     __device__ __forceinline__ static unsigned running_sum(unsigned v) {
@@ -295,6 +296,7 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
         t.s.start = t.s.length - t.s.rows;
         count = __builtin_amdgcn_readlane(cuts, at);
         const unsigned in = item - __builtin_amdgcn_readlane(upto - mine, at);
+        if (in >= (unsigned)__builtin_amdgcn_readlane(mine, at)) return;  // (more tiles than 32 bits count)
         // heads first, then pieces: neighbours read the same pages
         const unsigned rest = __builtin_amdgcn_readfirstlane(in / (unsigned)a.pool.kv_heads);
         head = in - rest * a.pool.kv_heads;
@@ -305,9 +307,9 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
         int base;
         KvFew<KS>::range_of(a, t.s.start, t.s.length, base);
         from = base + KS * (int)(piece * stretch);
-        to = from + KS * (int)stretch;
+        to = piece == count - 1 ? t.hi : from + KS * (int)stretch;
         if (from < (t.lo & ~(KS - 1))) from = t.lo & ~(KS - 1);
-        if (to > t.hi || piece == count - 1) to = t.hi;
+        if (to > t.hi) to = t.hi;
     }
 
     // this lane's row (of both halves) as the operand Q^T
