@@ -340,10 +340,10 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
     u32x4_t kf[SUBS * NF], vf[SUBS * NF];
     float scales[SUBS];  // (8 bits) of keys, then of values, one a lane
     int page[BLOCKS], next_page[BLOCKS];
-    // what the table says of the blocks from `at` on; of a block beyond what the tile sees, of the last one
+    // what the table says of the blocks from `at` on; of a block ahead of or beyond what the tile sees, whose page may be given up, of the first or last one
     auto find_pages = [&](int at, int (&p)[BLOCKS]) {
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) p[i] = kv_page_entry(a.pool, a.batch, t.s.b, at + 16 * i < t.hi ? at + 16 * i : t.hi - 1);
+        for (int i = 0; i < BLOCKS; ++i) p[i] = kv_page_entry(a.pool, a.batch, t.s.b, kv_clamp(at + 16 * i, t.lo & ~15, t.hi - 1));
     };
     auto load_keys = [&](int at, const int (&p)[BLOCKS]) {
 #pragma unroll
@@ -785,10 +785,9 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
     const int *const table = a.batch.pages + (long)t.s.b * a.batch.width;
     const long page_bytes = ((long)a.pool.kv_heads << a.pool.shift) * DP * C::ES, head_bytes = ((long)head << a.pool.shift) * DP * C::ES;
     const int in_page = (1 << a.pool.shift) - 1;
-    auto position = [&](int stage, int blk) {
-        const int p = first + stage * KEYS + 16 * blk;
-        return p < t.hi ? p : (t.hi - 1) & ~15;
-    };
+    const int lowest = t.lo & ~15, highest = (t.hi - 1) & ~15;
+    // (a block ahead of or beyond what the tile sees, whose page may be given up: the first or last one that it sees)
+    auto position = [&](int stage, int blk) { return kv_clamp(first + stage * KEYS + 16 * blk, lowest, highest); };
     auto look_up = [&](int stage) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) entry[i] = table[position(stage, (threadIdx.x + C::NT * i) / C::BLOCK_CHUNKS % BLOCKS) >> a.pool.shift];

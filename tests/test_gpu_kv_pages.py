@@ -1,4 +1,5 @@
-"""Attention of long chunks over tables with page numbers that are none: nothing of the page that stands in for them reaches a row."""
+"""Attention over tables with page numbers that are none: nothing of the page that stands in for them reaches a row, and those ahead
+of a window are not met."""
 
 import math
 
@@ -6,7 +7,7 @@ import pytest
 import torch
 
 from gpu_util import DEV
-from test_gpu_kv import ends, ints, siso  # noqa: F401
+from test_gpu_kv import Setup, ints, siso  # noqa: F401
 from test_gpu_kv_heavy import Wide
 
 pytestmark = pytest.mark.gpu
@@ -44,3 +45,24 @@ def test_scores_of_no_page_do_not_weigh(siso, dtype, d, rows, length, none, ther
     q = (1 + 0.1 * s.queries(1).float()).bfloat16()
     s.check(q, hidden={0: range(16 * none, 16 * none + 16)}, label="no page")
     assert s.kv.bad_pages() > 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("d,page,new,length", [(64, 16, [1, 4], [900, 333]), (64, 32, [150], [700]), (128, 16, [3, 1, 2], [2100, 60, 515]),
+                                               (128, 64, [270, 140], [1000, 300]), (192, 16, [1, 130], [777, 400]), (256, 16, [2], [450])])
+@pytest.mark.parametrize("window", [1, 17, 45, 100, 250])
+@pytest.mark.parametrize("kind", [Setup, Wide])
+def test_pages_given_up_ahead_of_a_window(siso, dtype, d, page, new, length, window, kind):  # noqa: F811
+    """Whoever keeps a window gives up the pages that no row sees any more: they are not met, and the bits are the same."""
+    print(f"case: pages given up {dtype} d={d} {page} {new} {length} {window} {kind.__name__}", flush=True)
+    s = kind(siso, dtype, d, 1, page, new, length, seed=121)
+    s.k[:2], s.v[:2] = math.nan, math.inf  # (of the first sequence, ahead of all windows)
+    s.write()
+    q = s.queries(2)
+    want = s.kv.attend(s.batch, q.to(DEV), window=window, with_lse=True)
+    for b, (m, l) in enumerate(zip(new, length)):
+        s.pages[b, :max(0, l - m - window + 1) // page] = -1
+    got = s.kv.attend(s.batch, q.to(DEV), window=window, with_lse=True)
+    assert s.kv.bad_pages() == 0
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    s.check(q, window=window, got=got, label="pages given up")
