@@ -42,7 +42,8 @@ typedef struct siso_kv siso_kv; /* opaque; owns the pages on the device */
  *   n:      sequences, at most 65,535;  rows: new tokens in all, at most 2^24.
  *   first:  device pointer, n + 1 ints, not decreasing, from 0 to rows.
  *   length: device pointer, n ints, 0 to width * page_tokens;
- *   pages:  device pointer, [n][width] page numbers (NULL length and pages: siso_kv_verify).
+ *   pages:  device pointer, [n][width] page numbers (NULL length and pages: siso_kv_verify);
+ *           width * page_tokens is at most 2^31 - 2^25 (SISO_EINVAL otherwise).
  *   max_new, max_length: no sequence has more new tokens / more tokens (0: not known; rows
  *           and width * page_tokens are taken).  They size launches: rows of a sequence
  *           beyond max_new are not served, max_length only weighs on speed.

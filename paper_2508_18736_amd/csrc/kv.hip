@@ -48,7 +48,7 @@ int kv_batch(siso_kv *kv, const char *call, int layer, const siso_kv_batch *batc
     if (layer >= 0) {
         if (layer >= kv->layers) return kv_fail(kv, SISO_EINVAL, "%s: layer %d of %d", call, layer, kv->layers);
         if (b.n > 0 && (!b.length || !b.pages)) return kv_fail(kv, SISO_EINVAL, "%s: no lengths or no pages", call);
-        if (b.width < 0 || b.width > 2147483647L / kv->page_tokens) return kv_fail(kv, SISO_EINVAL, "%s: %ld pages of a sequence", call, b.width);
+        if (b.width < 0 || b.width > SISO_KV_MOST / kv->page_tokens) return kv_fail(kv, SISO_EINVAL, "%s: %ld pages of a sequence", call, b.width);
         out->length = b.length;
         out->pages = b.pages;
         out->width = b.width;

@@ -27,6 +27,9 @@ struct KvPool {
     int dim, dp;
 };
 
+// Positions of a sequence, at most: kernels look up to some thousand positions ahead and up to 2^24 rows and a window back, in 32 bits.
+#define SISO_KV_MOST ((1L << 31) - (1L << 25))
+
 struct KvBatch {  // siso_kv_batch as kernels take it
     const int *first, *length, *pages;
     int n, rows;

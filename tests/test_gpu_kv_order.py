@@ -1,4 +1,7 @@
-"""First rows that decrease, which no batch may have: what such a call returns is not said, the calls behind it are as ever."""
+"""Batches that no caller may give: first rows that decrease (what such a call returns is not said, the calls behind it are as ever) and
+tables wider than kernels count."""
+
+import ctypes as C
 
 import pytest
 import torch
@@ -31,3 +34,23 @@ def test_calls_behind_rows_that_two_sequences_claim(siso, dtype, d, times):  # n
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
             s.check(q, got=got, label="behind")
     assert s.kv.bad_pages() == 0
+
+
+@pytest.mark.parametrize("page", [16, 1024])
+def test_tables_of_more_positions_than_kernels_count(siso, page):  # noqa: F811
+    """The widest table is taken (none of it beyond the length is read), one page more is refused by every call that takes one."""
+    kv = siso.PagedKV(1, 64, 2, page_tokens=page)
+    widest = (2 ** 31 - 2 ** 25) // page
+    first, length, pages = ints([0, 2]), ints([2]), ints([[1]])
+    x = torch.randn(2, 1, 64, device=DEV).bfloat16()
+    for width, rc in ((widest, siso.OK), (widest + 1, siso.EINVAL), ((2 ** 31 - 1) // page, siso.EINVAL)):
+        batch = siso._KvBatchStruct(n=1, rows=2, first=first.data_ptr(), length=length.data_ptr(), pages=pages.data_ptr(), width=width, max_new=0, max_length=0)
+        out = [torch.zeros_like(x) for _ in range(3)]
+        assert siso._lib.siso_kv_write(kv._h, 0, C.byref(batch), x.data_ptr(), 64, 64, x.data_ptr(), 64, 64) == rc
+        assert siso._lib.siso_kv_read(kv._h, 0, C.byref(batch), siso.BF16, out[0].data_ptr(), out[1].data_ptr()) == rc
+        assert siso._lib.siso_kv_attend(kv._h, 0, C.byref(batch), x.data_ptr(), 64, 64, 1, 0.125, 0, out[2].data_ptr(), None) == rc
+        if rc == siso.OK:
+            assert torch.equal(out[0], x) and torch.equal(out[1], x) and torch.equal(out[2][0], x[0])
+        else:
+            assert b"pages" in siso._lib.siso_kv_last_error(kv._h)
+    assert kv.bad_pages() == 0
