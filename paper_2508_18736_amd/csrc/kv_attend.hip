@@ -1216,7 +1216,7 @@ extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch
     // (zero as the smallest number: a score of minus infinity times it stays one)
     a.scale = fmaxf(fabsf(scale) * 1.44269504089f, 1.17549435e-38f);
     a.negate = scale < 0.f ? 0x80008000u : 0u;
-    a.window = window;
+    a.window = window < a.batch.most ? window : 0;  // (all that there can be; what a row at a position below zero would see cannot wrap)
     a.out = (bf16_t *)out;
     a.lse = lse;
     a.parts = kv->parts;
