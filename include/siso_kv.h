@@ -103,7 +103,7 @@ int siso_kv_read(siso_kv *kv, int layer, const siso_kv_batch *batch, int out_typ
  *   q:     device pointer, 16-bit rows, strides as for siso_kv_write.
  *   heads: a multiple of kv_heads, at most 128 of them for each; rows * heads at most 2^30
  *          (SISO_EINVAL otherwise).
- *   scale: finite.
+ *   scale: finite; scores have to stay within single precision's range.
  *   out:   device pointer, [rows][heads][head_dim], 16 bits, 16-byte aligned.
  *   lse:   device pointer, [rows][heads] floats, or NULL.
  * A row that sees nothing gets zeros and lse = -inf.  Infinities and NaN at positions that

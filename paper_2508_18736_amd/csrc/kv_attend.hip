@@ -1202,7 +1202,7 @@ extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch
     if (rc != SISO_OK) return rc;
     if (heads < 1 || heads % kv->kv_heads != 0 || heads / kv->kv_heads > 128)
         return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: %d heads over %d kv heads", heads, kv->kv_heads);
-    if (!(fabsf(scale) <= 3.0e38f) || window < 0) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: scale %g, window %d", (double)scale, window);
+    if (!isfinite(scale) || window < 0) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: scale %g, window %d", (double)scale, window);
     if ((long)a.batch.rows * heads > 1L << 30) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: %d rows of %d heads", a.batch.rows, heads);
     if (a.batch.n == 0 || a.batch.rows == 0) return SISO_OK;
     if (!q || !out || ((uintptr_t)q & 1) || ((uintptr_t)out & 15) || ((uintptr_t)lse & 3))
@@ -1213,8 +1213,8 @@ extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch
     a.q_head = q_head;
     a.vec = ((uintptr_t)q & 15) == 0 && q_token % 8 == 0 && q_head % 8 == 0;
     a.group = heads / kv->kv_heads;
-    // (zero as the smallest number: a score of minus infinity times it stays one)
-    a.scale = fmaxf(fabsf(scale) * 1.44269504089f, 1.17549435e-38f);
+    // (zero as the smallest number: a score of minus infinity times it stays one; and what would leave the range as the largest: a score of zero stays one)
+    a.scale = fminf(fmaxf(fabsf(scale) * 1.44269504089f, 1.17549435e-38f), 3.40282347e38f);
     a.negate = scale < 0.f ? 0x80008000u : 0u;
     a.window = window < a.batch.most ? window : 0;  // (all that there can be; what a row at a position below zero would see cannot wrap)
     a.out = (bf16_t *)out;
