@@ -1152,7 +1152,7 @@ static int attend_chunks(siso_kv *kv, const KvAttend &a) {
     if (ways < 1) ways = 1;
     p.ways = (int)ways;
     if (C::LDS > 64 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_attend_chunk<DP, FP8>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS));
-    const long slots = p.slots, piece = (1L << 23) / (kv->kv_heads * ways);  // (a launch has fewer than 2^32 threads)
+    const long slots = p.slots, piece = ((1L << 31) / C::NT) / (kv->kv_heads * ways);  // (a launch has fewer than 2^32 threads)
     for (p.slot0 = 0; p.slot0 < slots; p.slot0 += piece) {
         p.slots = slots - p.slot0 < piece ? slots - p.slot0 : piece;
         hipLaunchKernelGGL((k_kv_attend_chunk<DP, FP8>), dim3((unsigned)(p.slots * ways * kv->kv_heads)), dim3(C::NT), C::LDS, kv->stream, a, p);
