@@ -116,7 +116,7 @@ def answer(cache: siso.SisoCache, stored: Sequence[Sequence[int]], target: Targe
     kinds = ["hit" if f[1] else "near" if f[0] else "miss" for f in flags]
     ask = [b for b, kind in enumerate(kinds) if kind != "hit"]
     got, steps = serve(target, [prompts[b] for b in ask], [stored[idx[b]] if kinds[b] == "near" else None for b in ask], tokens, **how)
-    answers = [list(stored[i])[:tokens] for i in idx]
+    answers = [list(stored[i])[:tokens] if kind == "hit" else [] for i, kind in zip(idx, kinds)]  # (no stored answer behind a miss: the cache may be empty)
     for b, a in zip(ask, got):
         answers[b] = a
     return answers, kinds, steps

@@ -1,0 +1,30 @@
+"""What near_hit does before and around the model's steps, without a GPU."""
+
+import pytest
+import torch
+
+from test_kv_abi import siso  # noqa: F401
+
+
+class Lookup:
+    """Answers of a lookup that are given."""
+
+    def __init__(self, idx, flags):
+        self.idx, self.flags = torch.tensor(idx), torch.tensor(flags)
+
+    def lookup_multi(self, queries, thetas, count_index):
+        return self.idx, None, self.flags
+
+
+def test_an_empty_cache_has_no_stored_answers(siso, monkeypatch):  # noqa: F811
+    from paper_2508_18736_amd import near_hit
+
+    asked = []
+    monkeypatch.setattr(near_hit, "serve", lambda target, prompts, drafts, tokens, **how: (asked.append((prompts, drafts)) or [[7] * tokens for _ in prompts], 3))
+    got = near_hit.answer(Lookup([-1, -1], [[0, 0], [0, 0]]), [], None, None, [[1], [2, 3]], 0.9, 0.7, 4)
+    assert got == ([[7] * 4, [7] * 4], ["miss", "miss"], 3)
+    assert asked == [([[1], [2, 3]], [None, None])]
+    # and beside others
+    got = near_hit.answer(Lookup([0, -1, 0], [[1, 1], [0, 0], [1, 0]]), [[5, 6, 8, 9, 9]], None, None, [[1], [2, 3], [4]], 0.9, 0.7, 4)
+    assert got == ([[5, 6, 8, 9], [7] * 4, [7] * 4], ["hit", "miss", "near"], 3)
+    assert asked[1] == ([[2, 3], [4]], [None, [5, 6, 8, 9, 9]])
