@@ -61,8 +61,8 @@ def serve(target: Target, prompts: Sequence[Sequence[int]], drafts: Sequence[Opt
     """``tokens`` tokens behind each prompt, and the number of the model's steps.  ``drafts[b]``: the stored answer of sequence b or
     None; at most ``most`` of its tokens are verified at a time.  Temperature 0: greedy."""
     n, dev = len(prompts), target.device
-    if n == 0:
-        return [], 0
+    if n == 0 or tokens <= 0:
+        return [[] for _ in prompts], 0
     need = [-(-(len(p) + tokens + most) // page_tokens) for p in prompts]
     kv = siso.PagedKV(target.kv_heads, target.head_dim, sum(need), page_tokens=page_tokens, layers=len(target.layers), dtype=dtype, device=dev)
     pages = torch.zeros(n, max(need), dtype=torch.int32)

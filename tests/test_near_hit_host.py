@@ -28,3 +28,11 @@ def test_an_empty_cache_has_no_stored_answers(siso, monkeypatch):  # noqa: F811
     got = near_hit.answer(Lookup([0, -1, 0], [[1, 1], [0, 0], [1, 0]]), [[5, 6, 8, 9, 9]], None, None, [[1], [2, 3], [4]], 0.9, 0.7, 4)
     assert got == ([[5, 6, 8, 9], [7] * 4, [7] * 4], ["hit", "miss", "near"], 3)
     assert asked[1] == ([[2, 3], [4]], [None, [5, 6, 8, 9, 9]])
+
+
+@pytest.mark.parametrize("tokens", [0, -1])
+def test_no_tokens_are_no_steps(siso, tokens):  # noqa: F811
+    from paper_2508_18736_amd import near_hit
+
+    target = near_hit.Target(layers=1, heads=2, vocab=50, device="cpu")
+    assert near_hit.serve(target, [[1, 2], [3]], [None, [4]], tokens) == ([[], []], 0)
