@@ -63,6 +63,8 @@ def serve(target: Target, prompts: Sequence[Sequence[int]], drafts: Sequence[Opt
     n, dev = len(prompts), target.device
     if n == 0 or tokens <= 0:
         return [[] for _ in prompts], 0
+    if not all(len(p) for p in prompts):
+        raise ValueError("prompts: every one has a token at least")
     need = [-(-(len(p) + tokens + most) // page_tokens) for p in prompts]
     kv = siso.PagedKV(target.kv_heads, target.head_dim, sum(need), page_tokens=page_tokens, layers=len(target.layers), dtype=dtype, device=dev)
     pages = torch.zeros(n, max(need), dtype=torch.int32)

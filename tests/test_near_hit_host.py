@@ -36,3 +36,11 @@ def test_no_tokens_are_no_steps(siso, tokens):  # noqa: F811
 
     target = near_hit.Target(layers=1, heads=2, vocab=50, device="cpu")
     assert near_hit.serve(target, [[1, 2], [3]], [None, [4]], tokens) == ([[], []], 0)
+
+
+def test_a_prompt_without_tokens_is_refused(siso):  # noqa: F811
+    from paper_2508_18736_amd import near_hit
+
+    target = near_hit.Target(layers=1, heads=2, vocab=50, device="cpu")
+    with pytest.raises(ValueError):
+        near_hit.serve(target, [[1, 2], []], [None, None], 3)
