@@ -149,13 +149,13 @@ def main() -> None:
     args = ap.parse_args()
     target = Target()
     cache, stored, queries, prompts = example(target, args.tokens)
-    answers, kinds, steps = answer(cache, stored, target, queries, prompts, 0.9, 0.7, args.tokens, most=args.drafts,
-                                   dtype=siso.FP8 if args.storage == "fp8" else siso.BF16, temperature=args.temperature)
+    how = dict(most=args.drafts, dtype=siso.FP8 if args.storage == "fp8" else siso.BF16, temperature=args.temperature)
+    answers, kinds, steps = answer(cache, stored, target, queries, prompts, 0.9, 0.7, args.tokens, **how)
     for b, kind in enumerate(kinds):
         same = sum(x == y for x, y in zip(answers[b], stored[b]))
         print(f"query {b}: {kind:4s} prompt of {len(prompts[b])} tokens, {same} of {len(answers[b])} tokens as in the stored answer")
     near = [b for b, kind in enumerate(kinds) if kind == "near"]
-    _, alone = serve(target, [prompts[b] for b in near], [stored[b] for b in near], args.tokens, most=args.drafts)
+    _, alone = serve(target, [prompts[b] for b in near], [stored[b] for b in near], args.tokens, **how)
     print(f"{len(kinds)} queries, {kinds.count('hit')} hits, {kinds.count('near')} near hits; {steps} steps for all that missed, "
           f"{alone} for the near hits, {args.tokens} without drafts")
 

@@ -44,3 +44,24 @@ def test_a_prompt_without_tokens_is_refused(siso):  # noqa: F811
     target = near_hit.Target(layers=1, heads=2, vocab=50, device="cpu")
     with pytest.raises(ValueError):
         near_hit.serve(target, [[1, 2], []], [None, None], 3)
+
+
+def test_the_command_serves_all_its_calls_alike(siso, monkeypatch, capsys):  # noqa: F811
+    """The steps that are printed side by side are steps of one storage and one temperature."""
+    import sys
+
+    from paper_2508_18736_amd import near_hit
+
+    calls = []
+
+    def serve(target, prompts, drafts, tokens, **how):
+        calls.append(how)
+        return [[1] * tokens for _ in prompts], 2
+
+    monkeypatch.setattr(near_hit, "serve", serve)
+    monkeypatch.setattr(near_hit, "Target", lambda: None)
+    monkeypatch.setattr(near_hit, "example", lambda target, tokens: (Lookup([0, 0], [[1, 0], [0, 0]]), [[1] * 5] * 2, None, [[1], [2]]))
+    monkeypatch.setattr(sys, "argv", ["near_hit", "--storage", "fp8", "--temperature", "0.5", "--drafts", "3", "--tokens", "5"])
+    near_hit.main()
+    assert calls == [dict(most=3, dtype=siso.FP8, temperature=0.5)] * 2
+    assert "1 near hits; 2 steps" in capsys.readouterr().out
