@@ -338,7 +338,8 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
     float m = -INFINITY, l = 0.f;
 
     u32x4_t kf[SUBS * NF], vf[SUBS * NF];
-    float scales[SUBS];  // (8 bits) of keys, then of values, one a lane
+    static_assert(!FP8 || KS == 32, "a lane for each key's scale, one for each value's");
+    float scale;  // (8 bits) a key's, in the other half of the lanes a value's
     int page[BLOCKS], next_page[BLOCKS];
     // what the table says of the blocks from `at` on; of a block ahead of or beyond what the tile sees, whose page may be given up, of the first or last one
     auto find_pages = [&](int at, int (&p)[BLOCKS]) {
@@ -363,11 +364,7 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
                 from_s = key >> 4 == i ? x : from_s;
             }
             from_s += key & 15;
-            if constexpr (SUBS == 1) scales[0] = (h ? a.pool.vs : a.pool.ks)[from_s];
-            else {
-                scales[0] = a.pool.ks[from_s];
-                scales[1] = a.pool.vs[from_s];
-            }
+            scale = (h ? a.pool.vs : a.pool.ks)[from_s];
         }
     };
     auto load_values = [&](int at, const int (&p)[BLOCKS]) {
@@ -398,8 +395,7 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
             }
         }
         if constexpr (FP8) {  // a lane has one position's scales and needs those of its registers': through LDS
-#pragma unroll
-            for (int i = 0; i < SUBS; ++i) sh_scales[64 * i + lane] = scales[i];
+            sh_scales[lane] = scale;
 #pragma unroll
             for (int g = 0; g < 4 * SUBS; ++g) {
                 const float4 x = *(const float4 *)(sh_scales + 8 * g + 4 * h);
