@@ -80,7 +80,8 @@ int siso_kv_set_stream(siso_kv *kv, void *hip_stream);
  * Keys and values of the batch's rows into layer `layer`.
  *   k, v: device pointers, 16-bit rows: element e of head h of row r at
  *         [r * token_stride + h * head_stride + e] (strides in elements, any).
- * A position that two rows of a batch name holds either's values.  Asynchronous.
+ * No two rows of a batch may name one position: elements of both, in 8 bits also the scale of one beside codes of the other,
+ * may stand there until it is written again.  Asynchronous.
  */
 int siso_kv_write(siso_kv *kv, int layer, const siso_kv_batch *batch, const void *k, long k_token_stride, long k_head_stride,
                   const void *v, long v_token_stride, long v_head_stride);
