@@ -713,7 +713,7 @@ __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces 
     const long j = slot - kv_slots_before(t.s.first, t.s.b, a.group, SHIFT, 1), work = (long)t.s.rows * a.group;
     if (j < 0 || j * ROWS >= work || work <= a.few) return false;
     kv_tile(a, (int)(j * ROWS), ROWS, t);
-    from = t.lo & ~(KEYS - 1);
+    from = t.lo & ~15;  // (no block that nobody sees: its page may be given up)
     blocks = t.hi > from ? (t.hi - from + KEYS - 1) / KEYS : 0;
     per = (blocks + p.ways - 1) / p.ways;
     if (per < KV_PIECE_LEAST / KEYS) per = KV_PIECE_LEAST / KEYS;
@@ -781,9 +781,10 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
     const int *const table = a.batch.pages + (long)t.s.b * a.batch.width;
     const long page_bytes = ((long)a.pool.kv_heads << a.pool.shift) * DP * C::ES, head_bytes = ((long)head << a.pool.shift) * DP * C::ES;
     const int in_page = (1 << a.pool.shift) - 1;
-    const int lowest = t.lo & ~15, highest = (t.hi - 1) & ~15;
-    // (a block ahead of or beyond what the tile sees, whose page may be given up: the first or last one that it sees)
-    auto position = [&](int stage, int blk) { return kv_clamp(first + stage * KEYS + 16 * blk, lowest, highest); };
+    auto position = [&](int stage, int blk) {
+        const int p = first + stage * KEYS + 16 * blk;
+        return p < t.hi ? p : (t.hi - 1) & ~15;
+    };
     auto look_up = [&](int stage) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) entry[i] = table[position(stage, (threadIdx.x + C::NT * i) / C::BLOCK_CHUNKS % BLOCKS) >> a.pool.shift];
