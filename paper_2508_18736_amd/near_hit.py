@@ -61,6 +61,8 @@ def serve(target: Target, prompts: Sequence[Sequence[int]], drafts: Sequence[Opt
     """``tokens`` tokens behind each prompt, and the number of the model's steps.  ``drafts[b]``: the stored answer of sequence b or
     None; at most ``most`` of its tokens are verified at a time.  Temperature 0: greedy."""
     n, dev = len(prompts), target.device
+    if most < 0:
+        raise ValueError(f"most: {most} drafted tokens at a time")
     if n == 0 or tokens <= 0:
         return [[] for _ in prompts], 0
     if not all(len(p) for p in prompts):

@@ -65,3 +65,11 @@ def test_the_command_serves_all_its_calls_alike(siso, monkeypatch, capsys):  # n
     near_hit.main()
     assert calls == [dict(most=3, dtype=siso.FP8, temperature=0.5)] * 2
     assert "1 near hits; 2 steps" in capsys.readouterr().out
+
+
+def test_fewer_drafts_than_none_are_refused(siso):  # noqa: F811
+    from paper_2508_18736_amd import near_hit
+
+    target = near_hit.Target(layers=1, heads=2, vocab=50, device="cpu")
+    with pytest.raises(ValueError):
+        near_hit.serve(target, [[1, 2]], [[3, 4]], 3, most=-1)
