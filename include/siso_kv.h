@@ -45,8 +45,8 @@ typedef struct siso_kv siso_kv; /* opaque; owns the pages on the device */
  *   pages:  device pointer, [n][width] page numbers (NULL length and pages: siso_kv_verify);
  *           width * page_tokens is at most 2^31 - 2^25 (SISO_EINVAL otherwise).
  *   max_new, max_length: no sequence has more new tokens / more tokens (0: not known; rows
- *           and width * page_tokens are taken).  They size launches: rows of a sequence
- *           beyond max_new are not served, max_length only weighs on speed.
+ *           and width * page_tokens are taken).  They size launches: a sequence of more rows
+ *           than max_new may be left out, max_length only weighs on speed.
  * The arrays are read when the work runs.  What does not keep to these ranges is never
  * read or written at: lengths are taken as the closest allowed one, positions below 0 are
  * no positions (nothing is written; a query there sees nothing), and a page number that
