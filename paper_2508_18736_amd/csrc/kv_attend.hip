@@ -118,7 +118,8 @@ __device__ __forceinline__ void kv_finish(const KvAttend &a, const KvTile &t, in
 #define KV_LIGHT (1L << 26)
 #define KV_LIGHT_MIXED (1L << 30)
 #define KV_STRETCHES 1024
-#define KV_LEAST 4  // units of a stretch, at least: one for each wave
+#define KV_LEAST 4  // units of a stretch, at least, one for each wave (one token of 2,001 positions gets 5: the launch has no workgroup for the last part of 4, and the fifth
+                    // unit is a second step of one wave)
 #define KV_ENOUGH 32 // units that are worth being joined
 #define KV_FULL 256  // workgroups
 #define KV_PLAN_CHUNKS 1024  // 65,535 sequences, 64 each
@@ -238,8 +239,9 @@ __global__ __launch_bounds__(1024) void k_kv_plan(KvAttend a) {
 // TB/s (a large copy on the same card: 5.0), two over 232,244 in 16 bits, 951 MB, in 177 us, 5.4 TB/s.  Short ones are bound by latency: one
 // token over 2,001 positions takes 10 us, of which the join is about 3.
 // Up to 64 elements a step of 64 positions, where two waves on a SIMD unit have to have enough on their way (24 sequences of up to 12 rows and 30,000
-// positions, 16 bits: 36 us; steps of 32 and three waves 40, four 48), but of codes, which are half the bytes, 32 and four waves (the
-// same 25 and 25 us; 5,261 rows of 40 sequences under a window of 1,000, 12 heads: 49 and 38).
+// positions, 16 bits: 36 us; steps of 32 and three waves 40, four 48), but of codes, which are half the bytes, 32 and four waves (with 64 and two
+// 25 and 25 us; 5,261 rows of 40 sequences under a window of 1,000, 12 heads: 49 and 38; 250 rows over 4,000, 16 heads over 4: 24.0 and 17.8.  It
+// costs where there are few workgroups: 60 rows over 4,000 12.1 and 14.3 us, 400 rows 23.1 and 26.2).
 template <int DP, bool FP8>
 constexpr int kv_step() { return DP <= 64 && !FP8 ? 64 : 32; }
 template <int DP, bool FP8>
@@ -458,6 +460,9 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
 #pragma unroll
                 for (int r = 0; r < 16 * SUBS; ++r) s[r >> 4][r & 15] = seen[r >> 4] >> (r & 15) & 1 ? s[r >> 4][r & 15] : 0.f;  // (the scale there may be NaN)
         }
+        // Powers are rounded to 16 bits, the operands of the matrix cores' fast products (those of 32 bits have a sixteenth of the rate); the
+        // sum that they are divided by is of the unrounded ones.  In relation to the definition in 64 bits outputs are off by 0.0019 to 0.0024
+        // where rounding the outputs alone leaves 0.0017.
         bf16x8_t pf[BLOCKS];
 #pragma unroll
         for (int r = 0; r < 16 * SUBS; ++r) pf[r >> 3][r & 7] = (__bf16)s[r >> 4][r & 15];
@@ -670,7 +675,7 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
 // positions, in stages of KEYS.  A wave goes through a stage in two phases with a barrier behind each: one of products, the scores of the next
 // stage and the sums of this one, and one of powers, of the next stage's scores.  Both take about as long, the one on the matrix cores, the
 // other on the vector units, and of the two waves on a SIMD unit one is always a phase behind: each has the unit that the other leaves.
-// (4,096 rows of 32 heads of 128 behind 8,193: 655 us, 1,050 TFLOP/s; in step, with one barrier a stage, both waited for the same unit: 785 us.)
+// (4,096 rows of 32 heads of 128 behind 8,193: 660 us, 1,040 TFLOP/s; in step, with one barrier a stage, both waited for the same unit: 785 us.)
 // Keys and values pass through LDS, two stages of each: keys are read a stage earlier than values.  A wave writes its share of the next ones
 // and asks for those after them in its phase of products, whose vector units are idle.  Codes become 16-bit numbers (exactly) on the way in.
 template <int DP, bool FP8>
@@ -903,6 +908,7 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
     };
     // A stage's phase of powers: its scores become operands of the products with its values.  Rows are weighed against the maximum of the first
     // stage in which they see something, as long as they can be (see below).
+    // (rounded to 16 bits for them, as in k_kv_attend_few)
     bf16x8_t pf[BLOCKS];
     float peak = -INFINITY;
     auto weigh = [&](int stage, f32x16_t (&s)[SUBS]) __attribute__((always_inline)) {

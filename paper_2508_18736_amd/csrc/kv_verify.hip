@@ -17,7 +17,8 @@ struct KvVerify {
 };
 #define KV_SLICES 256  // of a row, at most: one for each thread of the workgroup that joins them
 // Workgroups.  Drawing: as many as are on the chip at once (64 rows of 128,001 with a draft's: 22.2 us; 2,048 come in two turns, 25.5 us; 512:
-// 24.5).  Greedy, 64 sequences of 1 to 5 rows of 50,000: 13.5 us, 2,048 17.0; of 5 to 9 rows of 130,000 in 16 bits 38.5 and 31.3.
+// 24.5).  Greedy as many, whatever the rows: 64 sequences of 1 to 5 rows of 50,000: 13.3 us, 2,048 16.8; 250 rows of 65,537 in 16 bits 15.4 and 16.3; of
+// 5 to 9 rows of 130,000 52.3 and 52.9, in 16 bits 38.6 and 31.4: the largest batches would be served better by twice as many.
 #define KV_FILL 1024
 // Workgroups of a sequence, greedy: they count themselves at one address, one after the other (8 sequences of 1 to 9 rows of 128,000: 11.7 us; 128:
 // 14.0, as many as there are slices and rows: 21.5).
