@@ -16,6 +16,19 @@
  *   siso_kv_verify  judges drafted tokens by the target's probabilities, from random
  *                   numbers that the caller gives, and chooses the token that follows.
  *
+ * Several centroids may be close (siso_lookup_topk), and their stored answers differ: together
+ * they are a tree of drafted tokens, which the model reads at once.
+ *
+ *   siso_kv_tree         who is whose ancestor;
+ *   siso_kv_attend_tree  attention of the tree's rows: to the context and their ancestors;
+ *   siso_kv_verify_tree  which path of the tree stands, and the token that follows;
+ *   siso_kv_keep         moves that path's keys and values behind the context.
+ *
+ * A context that grows without bound is cut down to the positions that attention weighs:
+ *
+ *   siso_kv_weigh   adds up the attention weight of every position;
+ *   siso_kv_evict   keeps the positions with the largest sums, the newest and the first.
+ *
  * Conventions are those of siso.h: device pointers owned by the caller, all work enqueued
  * on the stream of siso_kv_set_stream, SISO_OK or a negative code, a message for the last
  * failure, calls on one handle not thread-safe against each other.  No call but
@@ -148,6 +161,103 @@ int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch, const voi
 int siso_kv_verify(siso_kv *kv, const siso_kv_batch *batch, const int *tokens, int vocab, int type, const void *target,
                    long target_stride, const void *draft, long draft_stride, const float *u_accept, const float *u_sample,
                    int *out_accepted, int *out_tokens);
+
+/*
+ * A tree of drafted tokens.  The rows of a sequence are the tokens that the model is given at
+ * once: rows that continue the context, and rows that continue an earlier row, their parent.
+ *   parent:    device pointer, [rows] ints: of row i of a sequence the row of the same
+ *              sequence (0 to i - 1) that it continues; anything else: the context.
+ *   out_mask:  device pointer, [rows][SISO_KV_TREE / 32] words, 16-byte aligned: bit j % 32 of
+ *              word j / 32 is set for the row itself and for its ancestors j.
+ *   out_depth: device pointer, [rows] ints, or NULL: how many ancestors the row has: it
+ *              stands at position length - m + depth, though its keys and values
+ *              lie at length - m + i, as siso_kv_write puts them.
+ * Sequences of more than SISO_KV_TREE rows are left out, here and in the two calls below (SISO_EINVAL
+ * where max_new, or rows if it is 0, says that there may be one).  length and pages are
+ * not read.  Asynchronous.
+ */
+#define SISO_KV_TREE 256
+int siso_kv_tree(siso_kv *kv, const siso_kv_batch *batch, const int *parent, unsigned *out_mask, int *out_depth);
+
+/*
+ * siso_kv_attend for the rows of trees: row i of the m rows of a sequence of length L sees the
+ * positions before L - m and of the others those whose row is in its mask (bits of rows behind i
+ * are not looked at; any mask will do, one of siso_kv_tree makes a tree).  With a window > 0 it
+ * stands at P = L - m + d, d + 1 the number of its rows seen (d = 0 for none), and sees the
+ * positions j < L - m with j > P - window, and the last `window` rows of its mask.
+ *   mask: device pointer, [rows][SISO_KV_TREE / 32] words, 16-byte aligned.
+ * All else is as for siso_kv_attend.
+ */
+int siso_kv_attend_tree(siso_kv *kv, int layer, const siso_kv_batch *batch, const unsigned *mask, const void *q, long q_token_stride,
+                        long q_head_stride, int heads, float scale, int window, void *out, float *lse);
+
+/*
+ * Verification of a tree of drafted tokens.  Row 0 of a sequence is the last token that stands, the rows that continue it are
+ * the first drafted ones, and so on (a row other than 0 that continues nothing is never come to).  The walk begins
+ * at row 0: the target's distribution behind a row names a token; if a row that continues this one has that
+ * token (the first of several), the walk goes on there, otherwise it ends and the token is the one that follows.
+ *   parent:  as for siso_kv_tree;  tokens, vocab, type, target: as for siso_kv_verify.
+ *   u:       device pointer, [rows] floats in [0, 1): behind row r the first token is named at which the
+ *            running sum of target's row exceeds u[r] times its sum (weights below zero and NaN count as zero;
+ *            a row without any weight names -1, which no row has).  So the tokens are distributed
+ *            as the target's own, whatever the tree.  NULL: greedy, the largest entry (the lowest index of
+ *            equal ones, NaN never): target may hold logits.
+ *   out_accepted: device pointer, [n] ints: drafted tokens that stand (-1: a sequence without rows).
+ *   out_rows:     device pointer, [rows] ints: per sequence the rows of the walk, 0 first, then -1.
+ *   out_tokens:   device pointer, [rows] ints: per sequence the tokens that stand, the token that follows, then -1.
+ * With that, and siso_kv_keep, the sequence stands at length[b] - m + 1 + out_accepted[b] tokens.
+ * Only rows that the walk comes to are read.  Sums are formed in double precision.  Asynchronous.
+ */
+int siso_kv_verify_tree(siso_kv *kv, const siso_kv_batch *batch, const int *parent, const int *tokens, int vocab, int type,
+                        const void *target, long target_stride, const float *u, int *out_accepted, int *out_rows, int *out_tokens);
+
+/*
+ * The path of a tree that stands: the keys and values of row path[j] of a sequence, j = 0, 1, ..., move
+ * to the place of row j, in layer `layer`, or with -1 in all of them by one call.
+ *   path: device pointer, [rows] ints, as siso_kv_verify_tree leaves out_rows: increasing, with
+ *         path[j] >= j (what does not keep to that ends it).
+ * A sequence's pages from the one of its first row on are its own.  Asynchronous.
+ */
+int siso_kv_keep(siso_kv *kv, int layer, const siso_kv_batch *batch, const int *path);
+
+/*
+ * Attention weights, added up.  With the rows, heads and window of siso_kv_attend and the lse that it left, every position j of
+ * a sequence has in each kv head h
+ *     mass = (j < fresh ? decay * mass : 0) + sum of exp(scale * <q, k_j> - lse)
+ * over the batch's rows of the sequence that see j and the query heads that share h.  Positions from `fresh` on begin
+ * at zero, and are noted as those up to `newest`: born = newest - (length - 1 - j).
+ *   lse:    device pointer, [rows][heads] floats; a row whose lse is -inf (it saw nothing) adds nothing.
+ *   fresh:  device pointer, [n] ints, or NULL: length - m of each, the batch's rows are new.  (0: all that was
+ *           noted is forgotten, for instance where a prompt's last tokens weigh all of it.)
+ *   newest: device pointer, [n] ints, or NULL: length - 1 of each.  Where positions have been evicted, the true
+ *           position of the newest token.
+ *   decay:  0 to 1.  1: sums over all rows so far; 0: of this batch's rows alone.
+ *   mass:   device pointer, [layers][pages][kv_heads][page_tokens] floats: a position's is that of its slot.
+ *   born:   the same of ints, or NULL.
+ * A sequence without rows is left as it is, and so is all beyond its length.  No two sequences of a
+ * batch may share a page.  Scores and sums are formed in single precision, the sums in an order that does not
+ * depend on scheduling.  Asynchronous.
+ */
+int siso_kv_weigh(siso_kv *kv, int layer, const siso_kv_batch *batch, const void *q, long q_token_stride, long q_head_stride, int heads,
+                  float scale, int window, const float *lse, const int *fresh, const int *newest, float decay, float *mass, int *born);
+
+/*
+ * Eviction.  Of every sequence of more than `keep` positions each kv head keeps `keep`: first those whose born is
+ * among the newest `recent` (above the largest born of the sequence and head, minus recent) or below `early`, then those
+ * of the largest mass; of equal ones the lowest slots (NaN counts as less than all else).  Those that stand
+ * below `keep` stay where they are, the others go, in order, to the places that become free: keys, values, mass and born.  So
+ * heads keep unlike positions, and their order is no longer that of the tokens, which attention does not
+ * ask for (a window counts slots).  The sequence then stands at min(length, keep) positions.
+ *   layer:  or -1: all, by one call.  batch: its rows are not looked at.
+ *   keep:   1 to 2^23;  recent, early: from 0 on, together at most keep.
+ *   mass:   as for siso_kv_weigh;  born: too, or NULL: a slot's number stands for it.
+ *   to:     NULL: in place.  Or a device pointer, [n][to_width] page numbers: what is kept, or all of a sequence of
+ *           at most `keep` positions, goes there, mass and born too, and what the batch's pages hold stays as it is
+ *           (for pages that others share).  No page may be in both; slots beyond to_width pages are left out.
+ * No two sequences of a batch may share a page that is written.  Asynchronous.
+ */
+int siso_kv_evict(siso_kv *kv, int layer, const siso_kv_batch *batch, long keep, long recent, long early, float *mass, int *born,
+                  const int *to, long to_width);
 
 /* Page numbers outside the cache that calls have met since it was created (each counted at least once per call and layer).
  * Synchronises with the stream.  Negative = error code. */

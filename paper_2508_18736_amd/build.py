@@ -17,7 +17,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsiso.so")
 
 SOURCES = ["siso.hip", "lookup_mfma.hip", "lookup_few.hip", "lookup_bytes.hip", "lookup_tile.hip", "screen.hip", "topk.hip", "fp8.hip", "refresh.hip", "cluster.hip", "probe.hip",
-           "kv.hip", "kv_attend.hip", "kv_verify.hip"]
+           "kv.hip", "kv_attend.hip", "kv_verify.hip", "kv_tree.hip", "kv_weigh.hip", "kv_evict.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",

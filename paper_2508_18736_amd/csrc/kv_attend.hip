@@ -1,4 +1,4 @@
-// Attention over the paged cache (siso_kv_attend).  Layout of the pages: kv_internal.h.
+// Attention over the paged cache (siso_kv_attend, siso_kv_attend_tree).  Layout of the pages: kv_internal.h.
 #include <math.h>
 #include <type_traits>
 
@@ -27,6 +27,7 @@ struct KvAttend {
     unsigned *arrived;  // [2 * KV_STRETCHES]: parts of a tile that are there, by the number of its first; zeros between calls
     struct KvPlan *plan;
     long item0, items;  // of this launch the first; how many there may be
+    const unsigned *mask;  // of a tree's rows, [rows][KV_MASK_WORDS]
 };
 
 struct KvTile {
@@ -38,15 +39,63 @@ struct KvTile {
 __device__ __forceinline__ int kv_window_from(const KvAttend &a, int pos) {  // the first position that a row at `pos` sees
     return a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
 }
+// A tree's rows stand at most as deep as they lie: of what lies behind the context a row sees what its mask has.
+template <bool TREE>
 __device__ __forceinline__ void kv_tile(const KvAttend &a, int row0, int size, KvTile &t) {
     const int work = t.s.rows * a.group;  // (2^30 at most)
     t.row0 = row0;
     t.rows = work - row0 < size ? work - row0 : size;
     const int first = t.s.start + row0 / a.group, last = t.s.start + (row0 + t.rows - 1) / a.group;
     t.hi = last + 1 > 0 ? last + 1 : 0;
-    t.lo = kv_window_from(a, first);
-    t.all_hi = first + 1;
+    t.lo = kv_window_from(a, TREE ? t.s.start : first);
+    t.all_hi = TREE ? t.s.start : first + 1;
     t.all_lo = kv_window_from(a, last);
+}
+
+// A row's mask in LDS: a word of ones (of the context), the words, a word of zeros; rows lie so that lanes meet in no bank.
+#define KV_MASK_WORDS (SISO_KV_TREE / 32)
+#define KV_MASK_ROW (KV_MASK_WORDS + 3)
+// Lanes l and l + 32 bring the row of work of lane l: half of its words each.  A window leaves it the last `window` rows of its own.  Returns
+// its depth.  Only lanes of one wave share what is written here.
+__device__ __forceinline__ int kv_mask_row(const KvAttend &a, const KvTile &t, int token, bool valid, unsigned *lds) {
+    constexpr int HALF = KV_MASK_WORDS / 2;
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    u32x4_t w = u32x4_t{0, 0, 0, 0};
+    static_assert(HALF == 4, "16 bytes for a lane");
+    if (valid) w = *(const u32x4_t *)(a.mask + (size_t)(t.s.first + token) * KV_MASK_WORDS + HALF * h);
+    int seen = 0;
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) {  // (no row behind this one)
+        const int over = token + 1 - 32 * (HALF * h + i);
+        w[i] &= over >= 32 ? 0xFFFFFFFFu : over <= 0 ? 0u : (1u << over) - 1u;
+        seen += __popc(w[i]);
+    }
+    const int upper = __shfl(seen, n + 32), lower = __shfl(seen, n);
+    const int depth = upper + lower > 0 ? upper + lower - 1 : 0;
+    if (a.window > 0) {
+        int drop = upper + lower - a.window;  // the first so many of the row's
+        if (h) drop -= lower;
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) {
+            const int has = __popc(w[i]);
+            if (drop >= has) w[i] = 0;
+            else
+                for (int k = 0; k < drop; ++k) w[i] &= w[i] - 1;
+            drop -= has;
+        }
+    }
+    unsigned *const row = lds + n * KV_MASK_ROW;
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) row[1 + HALF * h + i] = w[i];
+    row[h ? KV_MASK_WORDS + 1 : 0] = h ? 0u : 0xFFFFFFFFu;
+    return depth;
+}
+// Bits of 32 positions, the first of them `off` (the same in every lane) behind the tree's first row: what lies ahead of that is the context.
+__device__ __forceinline__ unsigned kv_mask_bits(const unsigned *lds, int row, int off) {
+    if (off < -32) return 0xFFFFFFFFu;
+    if (off >= SISO_KV_TREE) return 0u;
+    const unsigned *w = lds + row * KV_MASK_ROW + 1 + (off >> 5);
+    return (unsigned)((((u64)w[1] << 32) | w[0]) >> (off & 31));
 }
 
 __device__ __forceinline__ bf16x8_t kv_as_bf16(u32x4_t x) { return __builtin_bit_cast(bf16x8_t, x); }
@@ -129,7 +178,7 @@ struct KvPlan {  // more than 64 sequences: made by a launch of its own
 };
 static_assert(sizeof(KvPlan) <= SISO_KV_PLAN_BYTES, "room for the plan");
 
-template <int KS>
+template <int KS, bool TREE>
 struct KvFew {
     int first, rows, length;  // of this lane's sequence
     int tiles, range;         // its tiles (of all kv heads; 0: not one of these sequences) and the units of each
@@ -145,7 +194,7 @@ struct KvFew {
         first = s.first;
         rows = s.rows;
         length = s.length;
-        if (rows == 0 || rows * a.group > a.few) return;
+        if (rows == 0 || rows * a.group > a.few || (TREE && rows > SISO_KV_TREE)) return;
         int from;
         tiles = ((rows * a.group + 31) >> 5) * a.pool.kv_heads;
         range = range_of(a, s.start, length, from);
@@ -178,12 +227,12 @@ __device__ __forceinline__ u64 kv_wave_sum(u64 v) {
 }
 
 // What every workgroup of k_kv_attend_few has to know of all sequences, where they are more than a wave takes in.
-template <int KS>
+template <int KS, bool TREE>
 __global__ __launch_bounds__(1024) void k_kv_plan(KvAttend a) {
     __shared__ u64 sums[32];
     __shared__ unsigned items[KV_PLAN_CHUNKS], parts[KV_PLAN_CHUNKS], waves[2][16];
     const int t = threadIdx.x, lane = t & 63, w = t >> 6, chunks = (a.batch.n + 63) / 64;
-    KvFew<KS> few;
+    KvFew<KS, TREE> few;
     u64 all = 0, all_tiles = 0;
     for (int b = t; b < a.batch.n; b += 1024) {
         few.load(a, b);
@@ -202,7 +251,7 @@ __global__ __launch_bounds__(1024) void k_kv_plan(KvAttend a) {
         all += sums[i];
         all_tiles += sums[16 + i];
     }
-    const unsigned stretch = KvFew<KS>::stretch_of(a, all, all_tiles);
+    const unsigned stretch = KvFew<KS, TREE>::stretch_of(a, all, all_tiles);
     for (int c = w; c < chunks; c += 16) {
         few.load(a, 64 * c + lane);
         const unsigned cuts = few.cuts(stretch), mine = few.tiles * cuts;
@@ -214,7 +263,7 @@ __global__ __launch_bounds__(1024) void k_kv_plan(KvAttend a) {
     }
     __syncthreads();
     const unsigned mine = t < chunks ? items[t] : 0, my_parts = t < chunks ? parts[t] : 0;
-    unsigned upto = KvFew<KS>::running_sum(mine), upto_parts = KvFew<KS>::running_sum(my_parts);
+    unsigned upto = KvFew<KS, TREE>::running_sum(mine), upto_parts = KvFew<KS, TREE>::running_sum(my_parts);
     if (lane == 63) {
         waves[0][w] = upto;
         waves[1][w] = upto_parts;
@@ -244,7 +293,7 @@ __global__ __launch_bounds__(1024) void k_kv_plan(KvAttend a) {
 // costs where there are few workgroups: 60 rows over 4,000 12.1 and 14.3 us, 400 rows 23.1 and 26.2).
 template <int DP, bool FP8>
 constexpr int kv_step() { return DP <= 64 && !FP8 ? 64 : 32; }
-template <int DP, bool FP8>
+template <int DP, bool FP8, bool TREE>
 __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void k_kv_attend_few(KvAttend a) {
     constexpr int ES = FP8 ? 1 : 2;
     constexpr int KS = kv_step<DP, FP8>(), SUBS = KS / 32, BLOCKS = KS / 16;
@@ -260,7 +309,8 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
     unsigned first_part;               // of the tile
     {
         const unsigned item = (unsigned)(a.item0 + blockIdx.x);
-        KvFew<KS> few;
+        using Few = KvFew<KS, TREE>;
+        Few few;
         unsigned stretch, items_before = 0, parts_before = 0;
         int chunk = 0;
         if (a.batch.n <= 64) {
@@ -270,7 +320,7 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
                 all = kv_wave_sum(all);
                 all_tiles = kv_wave_sum(all_tiles);
             }
-            stretch = __builtin_amdgcn_readfirstlane(KvFew<KS>::stretch_of(a, all, all_tiles));
+            stretch = __builtin_amdgcn_readfirstlane(Few::stretch_of(a, all, all_tiles));
         } else {  // the last 64 with no more items before them than this one
             int count = (a.batch.n + 63) / 64;
             while (count > 1) {
@@ -286,8 +336,8 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
             few.load(a, 64 * chunk + lane);
         }
         const unsigned cuts = few.cuts(stretch), mine = few.tiles * cuts, my_parts = cuts > 1 ? mine : 0;
-        const unsigned upto = items_before + (a.batch.n > 1 ? KvFew<KS>::running_sum(mine) : mine);
-        const unsigned upto_parts = parts_before + (a.batch.n > 1 ? KvFew<KS>::running_sum(my_parts) : my_parts);
+        const unsigned upto = items_before + (a.batch.n > 1 ? Few::running_sum(mine) : mine);
+        const unsigned upto_parts = parts_before + (a.batch.n > 1 ? Few::running_sum(my_parts) : my_parts);
         const u64 over = __ballot(upto > item);
         if (over == 0) return;  // (there are not as many items)
         const int at = __ffsll((long long)over) - 1;
@@ -305,9 +355,9 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
         const unsigned tile = __builtin_amdgcn_readfirstlane(rest / (unsigned)count);
         piece = rest - tile * count;
         first_part = __builtin_amdgcn_readlane(upto_parts - my_parts, at) + (tile * a.pool.kv_heads + head) * count;
-        kv_tile(a, tile * 32, 32, t);
+        kv_tile<TREE>(a, tile * 32, 32, t);
         int base;
-        KvFew<KS>::range_of(a, t.s.start, t.s.length, base);
+        Few::range_of(a, t.s.start, t.s.length, base);
         from = base + KS * (int)(piece * stretch);
         to = piece == count - 1 ? t.hi : from + KS * (int)stretch;
         if (from < (t.lo & ~(KS - 1))) from = t.lo & ~(KS - 1);
@@ -319,6 +369,10 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
     const bool valid = n < t.rows;
     const int pos = t.s.start + token;
     u32x4_t qx[DP / 16];
+    unsigned *const masks = (unsigned *)(sh + w * 32 * RS) + 64;  // (TREE) this wave's, behind its scales
+    static_assert(64 + 32 * KV_MASK_ROW <= 32 * RS, "room for the masks");
+    int depth = 0;
+    if constexpr (TREE) depth = kv_mask_row(a, t, valid ? token : 0, valid, masks);
     const bf16_t *const q_row = a.q + (long)(t.s.first + (valid ? token : 0)) * a.q_token + (long)(valid ? qh : 0) * a.q_head;
     auto q_at = [&](int s) { return FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h; };
     if (a.vec) {
@@ -420,10 +474,14 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub) {
                 seen[sub] = 0;
+                const unsigned own = TREE ? kv_mask_bits(masks, n, at + 32 * sub - t.s.start) >> 4 * h : 0u;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int p = at + 32 * sub + 8 * (r >> 2) + 4 * h + (r & 3);
-                    if (p <= pos && (a.window == 0 || p > pos - a.window) && kv_is_page(a.pool, page[2 * sub + (r >> 3)])) seen[sub] |= 1u << r;
+                    bool sees;
+                    if constexpr (TREE) sees = (own >> (8 * (r >> 2) + (r & 3)) & 1) && (a.window == 0 || p >= t.s.start || p > t.s.start + depth - a.window);
+                    else sees = p <= pos && (a.window == 0 || p > pos - a.window);
+                    if (sees && kv_is_page(a.pool, page[2 * sub + (r >> 3)])) seen[sub] |= 1u << r;
                     s[sub][r] = seen[sub] >> r & 1 ? s[sub][r] : -INFINITY;
                 }
             }
@@ -694,7 +752,8 @@ struct KvChunk {
     static constexpr int SCALES = 4 * HALF;                // (8 bits) where the scales begin: of four stages, keys' and values'
     static constexpr int FOUND = SCALES + (FP8 ? 4 * 2 * KEYS * 4 : 0);  // three words: a value that is not finite, a maximum that grew too far, a page that is none
     static constexpr int LDS = FOUND + 16 + 4 * BLOCKS * 4;  // and which blocks of four stages have a page
-    static_assert(LDS <= 160 * 1024 && NT >= 2 * KEYS, "fits LDS; a thread for each scale");
+    static constexpr int MASKS = ROWS * KV_MASK_ROW * 4;     // (trees) behind that
+    static_assert(LDS + MASKS <= 160 * 1024 && NT >= 2 * KEYS, "fits LDS; a thread for each scale");
 };
 #define KV_CHUNK_PART(ROWS, DP) ((size_t)(ROWS) * ((DP) + 2))
 
@@ -710,14 +769,14 @@ struct KvPieces {
 // and products may not.  (Nothing bounded, the compiler moves operands' reads to where they are waited for: 8% slower.)
 #define KV_MASK 0x276
 // The tile of a slot, of `rows` rows of work, and how its positions are cut: pieces of `per` blocks of KEYS positions from `from` on.
-template <int ROWS, int KEYS>
+template <int ROWS, int KEYS, bool TREE>
 __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces &p, long slot, KvTile &t, int &from, int &blocks, int &per, int &pieces) {
     constexpr int SHIFT = ROWS == 256 ? 8 : 7;
     static_assert(ROWS == 1 << SHIFT, "rows of a tile");
     t.s = kv_sequence_of(a.batch, slot, a.group, SHIFT, 1);
     const long j = slot - kv_slots_before(t.s.first, t.s.b, a.group, SHIFT, 1), work = (long)t.s.rows * a.group;
-    if (j < 0 || j * ROWS >= work || work <= a.few) return false;
-    kv_tile(a, (int)(j * ROWS), ROWS, t);
+    if (j < 0 || j * ROWS >= work || work <= a.few || (TREE && t.s.rows > SISO_KV_TREE)) return false;
+    kv_tile<TREE>(a, (int)(j * ROWS), ROWS, t);
     from = t.lo & ~15;  // (no block that nobody sees: its page may be given up)
     blocks = t.hi > from ? (t.hi - from + KEYS - 1) / KEYS : 0;
     per = (blocks + p.ways - 1) / p.ways;
@@ -726,7 +785,7 @@ __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces 
     return true;
 }
 
-template <int DP, bool FP8>
+template <int DP, bool FP8, bool TREE>
 __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD)) void k_kv_attend_chunk(KvAttend a, KvPieces p) {
     using C = KvChunk<DP, FP8>;
     constexpr int KEYS = C::KEYS, SUBS = C::SUBS, BLOCKS = C::BLOCKS, NS = C::NS, NU = C::NU, NL = C::NL;
@@ -737,18 +796,21 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
     const long slot = p.slot0 + p.slots - 1 - blockIdx.x / (a.pool.kv_heads * p.ways);
     KvTile t;
     int from, blocks, per, pieces;
-    if (!kv_chunk_tile<C::ROWS, KEYS>(a, p, slot, t, from, blocks, per, pieces) || piece >= pieces) return;
+    if (!kv_chunk_tile<C::ROWS, KEYS, TREE>(a, p, slot, t, from, blocks, per, pieces) || piece >= pieces) return;
     const int first = from + piece * per * KEYS, stages = blocks - piece * per < per ? blocks - piece * per : per;
 
     // this wave's rows; `any`: there are some
     const bool any = w * 32 < t.rows;
     KvTile mine;
     mine.s = t.s;
-    kv_tile(a, any ? t.row0 + w * 32 : t.row0, 32, mine);
+    kv_tile<TREE>(a, any ? t.row0 + w * 32 : t.row0, 32, mine);
     const int row = t.row0 + w * 32 + n;
     const bool valid = row < t.row0 + t.rows;
     const int token = valid ? row / a.group : 0, qh = head * a.group + (valid ? row % a.group : 0), pos = t.s.start + token;
     auto q_at = [&](int s) { return FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h; };
+    unsigned *const masks = (unsigned *)(lds + C::LDS) + w * 32 * KV_MASK_ROW;  // (TREE) this wave's
+    int depth = 0;
+    if constexpr (TREE) depth = kv_mask_row(a, t, token, valid, masks);
     u32x4_t qx[NS];
     {
         const bf16_t *q_row = a.q + (long)(t.s.first + token) * a.q_token + (long)qh * a.q_head;
@@ -921,10 +983,14 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub) {
                 seen[sub] = 0;
+                const unsigned own = TREE ? kv_mask_bits(masks, n, at + 32 * sub - t.s.start) >> 4 * h : 0u;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int p = at + 32 * sub + 8 * (r >> 2) + 4 * h + (r & 3);
-                    if (p <= pos && (a.window == 0 || p > pos - a.window) && (bits >> (2 * sub + (r >> 3)) & 1)) seen[sub] |= 1u << r;
+                    bool sees;
+                    if constexpr (TREE) sees = (own >> (8 * (r >> 2) + (r & 3)) & 1) && (a.window == 0 || p >= t.s.start || p > t.s.start + depth - a.window);
+                    else sees = p <= pos && (a.window == 0 || p > pos - a.window);
+                    if (sees && (bits >> (2 * sub + (r >> 3)) & 1)) seen[sub] |= 1u << r;
                     s[sub][r] = seen[sub] >> r & 1 ? s[sub][r] : -INFINITY;
                 }
             }
@@ -1066,7 +1132,9 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
 #pragma unroll 1
             for (int key = 0; key < 16; ++key) {
                 const int p = at + key;
-                const bool sees = p <= pos && (a.window == 0 || p > pos - a.window);
+                bool sees;
+                if constexpr (TREE) sees = (kv_mask_bits(masks, n, p - t.s.start) & 1) && (a.window == 0 || p >= t.s.start || p > t.s.start + depth - a.window);
+                else sees = p <= pos && (a.window == 0 || p > pos - a.window);
                 const bf16_t *v = block + (size_t)kv_half(key) * DP * 8 + kv_slot(key);
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
@@ -1114,14 +1182,14 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
 }
 
 // Joins the pieces of the tiles that were cut, in their order, four elements a thread.
-template <int DP, bool FP8>
+template <int DP, bool FP8, bool TREE>
 __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) {
     using C = KvChunk<DP, FP8>;
     const int head = blockIdx.x % a.pool.kv_heads;
     const long at_slot = blockIdx.x / a.pool.kv_heads;
     KvTile t;
     int from, blocks, per, pieces;
-    if (!kv_chunk_tile<C::ROWS, C::KEYS>(a, p, p.slot0 + p.slots - 1 - at_slot, t, from, blocks, per, pieces) || pieces <= 1) return;
+    if (!kv_chunk_tile<C::ROWS, C::KEYS, TREE>(a, p, p.slot0 + p.slots - 1 - at_slot, t, from, blocks, per, pieces) || pieces <= 1) return;
     const float *parts = a.parts + (size_t)(at_slot * p.ways * a.pool.kv_heads + head) * KV_CHUNK_PART(C::ROWS, DP);
     const size_t next = (size_t)a.pool.kv_heads * KV_CHUNK_PART(C::ROWS, DP);
     const int i = blockIdx.y * 256 + threadIdx.x;
@@ -1143,7 +1211,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) 
 // Workgroups that run at once on 256 compute units.
 static int kv_chunk_workgroups(int dp) { return dp == 64 ? 512 : 256; }
 
-template <int DP, bool FP8>
+template <int DP, bool FP8, bool TREE>
 static int attend_chunks(siso_kv *kv, const KvAttend &a) {
     using C = KvChunk<DP, FP8>;
     KvPieces p;
@@ -1154,28 +1222,29 @@ static int attend_chunks(siso_kv *kv, const KvAttend &a) {
     if (ways > 64) ways = 64;
     if (ways < 1) ways = 1;
     p.ways = (int)ways;
-    if (C::LDS > 64 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_attend_chunk<DP, FP8>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS));
+    constexpr int LDS = C::LDS + (TREE ? C::MASKS : 0);
+    if (LDS > 64 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_attend_chunk<DP, FP8, TREE>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
     const long slots = p.slots, piece = ((1L << 31) / C::NT) / (kv->kv_heads * ways);  // (a launch has fewer than 2^32 threads)
     for (p.slot0 = 0; p.slot0 < slots; p.slot0 += piece) {
         p.slots = slots - p.slot0 < piece ? slots - p.slot0 : piece;
-        hipLaunchKernelGGL((k_kv_attend_chunk<DP, FP8>), dim3((unsigned)(p.slots * ways * kv->kv_heads)), dim3(C::NT), C::LDS, kv->stream, a, p);
+        hipLaunchKernelGGL((k_kv_attend_chunk<DP, FP8, TREE>), dim3((unsigned)(p.slots * ways * kv->kv_heads)), dim3(C::NT), LDS, kv->stream, a, p);
         KV_TRY(kv, hipGetLastError());
         if (ways > 1) {
-            hipLaunchKernelGGL((k_kv_attend_join<DP, FP8>), dim3((unsigned)(p.slots * kv->kv_heads), C::ROWS * (DP / 4) / 256), dim3(256), 0, kv->stream, a, p);
+            hipLaunchKernelGGL((k_kv_attend_join<DP, FP8, TREE>), dim3((unsigned)(p.slots * kv->kv_heads), C::ROWS * (DP / 4) / 256), dim3(256), 0, kv->stream, a, p);
             KV_TRY(kv, hipGetLastError());
         }
     }
     return SISO_OK;
 }
 
-template <int DP, bool FP8>
+template <int DP, bool FP8, bool TREE>
 static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
     // Which sequences there are is known on the device only: where both kinds can be, both kernels are launched, and each leaves the other's.
     const long seen = a.window > 0 && a.window + 32L < max_length ? a.window + 32L : max_length;
     const long light = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads * seen;
     a.few = DP <= 128 && light * DP <= (a.batch.rows >= max_new * a.batch.n ? KV_LIGHT : KV_LIGHT_MIXED) ? 1 << 30 : KV_FEW;
     if (max_new * a.group > a.few) {
-        const int rc = attend_chunks<DP, FP8>(kv, a);
+        const int rc = attend_chunks<DP, FP8, TREE>(kv, a);
         if (rc != SISO_OK || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
     }
     constexpr int KS = kv_step<DP, FP8>();
@@ -1185,31 +1254,34 @@ static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
     a.item0 = 0;
     static_assert((size_t)2 * KV_STRETCHES * KV_PART(256) <= SISO_KV_PARTS && 2 * KV_STRETCHES <= SISO_KV_JOINS, "room for the parts");
     if (a.batch.n > 64) {
-        hipLaunchKernelGGL(k_kv_plan<KS>, dim3(1), dim3(1024), 0, kv->stream, a);
+        hipLaunchKernelGGL((k_kv_plan<KS, TREE>), dim3(1), dim3(1024), 0, kv->stream, a);
         KV_TRY(kv, hipGetLastError());
     }
     for (; a.item0 < items; a.item0 += piece) {  // (a launch has fewer than 2^32 threads)
         const dim3 grid((unsigned)(items - a.item0 < piece ? items - a.item0 : piece));
-        hipLaunchKernelGGL((k_kv_attend_few<DP, FP8>), grid, dim3(256), 0, kv->stream, a);
+        hipLaunchKernelGGL((k_kv_attend_few<DP, FP8, TREE>), grid, dim3(256), 0, kv->stream, a);
         KV_TRY(kv, hipGetLastError());
     }
     return SISO_OK;
 }
 
-extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch, const void *q, long q_token, long q_head, int heads,
-                              float scale, int window, void *out, float *lse) {
+template <bool TREE>
+static int attend(siso_kv *kv, const char *call, int layer, const siso_kv_batch *batch, const unsigned *mask, const void *q, long q_token, long q_head,
+                  int heads, float scale, int window, void *out, float *lse) {
     if (!kv) return SISO_EINVAL;
-    if (layer < 0) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: layer %d", layer);
+    if (layer < 0) return kv_fail(kv, SISO_EINVAL, "%s: layer %d", call, layer);
     KvAttend a;
-    const int rc = kv_batch(kv, "siso_kv_attend", layer, batch, &a.batch);
+    const int rc = kv_batch(kv, call, layer, batch, &a.batch);
     if (rc != SISO_OK) return rc;
+    if (TREE && kv_max_new(batch) > SISO_KV_TREE) return kv_fail(kv, SISO_EINVAL, "%s: trees of %ld rows", call, kv_max_new(batch));
     if (heads < 1 || heads % kv->kv_heads != 0 || heads / kv->kv_heads > 128)
-        return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: %d heads over %d kv heads", heads, kv->kv_heads);
-    if (!isfinite(scale) || window < 0) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: scale %g, window %d", (double)scale, window);
-    if ((long)a.batch.rows * heads > 1L << 30) return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: %d rows of %d heads", a.batch.rows, heads);
+        return kv_fail(kv, SISO_EINVAL, "%s: %d heads over %d kv heads", call, heads, kv->kv_heads);
+    if (!isfinite(scale) || window < 0) return kv_fail(kv, SISO_EINVAL, "%s: scale %g, window %d", call, (double)scale, window);
+    if ((long)a.batch.rows * heads > 1L << 30) return kv_fail(kv, SISO_EINVAL, "%s: %d rows of %d heads", call, a.batch.rows, heads);
     if (a.batch.n == 0 || a.batch.rows == 0) return SISO_OK;
     if (!q || !out || ((uintptr_t)q & 1) || ((uintptr_t)out & 15) || ((uintptr_t)lse & 3))
-        return kv_fail(kv, SISO_EINVAL, "siso_kv_attend: queries and outputs must be there, outputs 16-byte aligned");
+        return kv_fail(kv, SISO_EINVAL, "%s: queries and outputs must be there, outputs 16-byte aligned", call);
+    if (TREE && (!mask || ((uintptr_t)mask & 15))) return kv_fail(kv, SISO_EINVAL, "%s: masks must be there, 16-byte aligned", call);
     a.pool = kv_pool(kv, layer);
     a.q = (const bf16_t *)q;
     a.q_token = q_token;
@@ -1225,16 +1297,27 @@ extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch
     a.parts = kv->parts;
     a.arrived = kv->arrived;
     a.plan = (KvPlan *)kv->plan;
-    const long max_new = batch->max_new > 0 && batch->max_new < a.batch.rows ? batch->max_new : a.batch.rows;
+    a.mask = mask;
+    const long max_new = kv_max_new(batch);
     const long max_length = batch->max_length > 0 && batch->max_length < a.batch.most ? batch->max_length : a.batch.most;
     switch (kv->dp / 64 + (kv->dtype == SISO_FP8 ? 4 : 0)) {
-        case 1: return attend<64, false>(kv, a, max_length, max_new);
-        case 2: return attend<128, false>(kv, a, max_length, max_new);
-        case 3: return attend<192, false>(kv, a, max_length, max_new);
-        case 4: return attend<256, false>(kv, a, max_length, max_new);
-        case 5: return attend<64, true>(kv, a, max_length, max_new);
-        case 6: return attend<128, true>(kv, a, max_length, max_new);
-        case 7: return attend<192, true>(kv, a, max_length, max_new);
-        default: return attend<256, true>(kv, a, max_length, max_new);
+        case 1: return attend<64, false, TREE>(kv, a, max_length, max_new);
+        case 2: return attend<128, false, TREE>(kv, a, max_length, max_new);
+        case 3: return attend<192, false, TREE>(kv, a, max_length, max_new);
+        case 4: return attend<256, false, TREE>(kv, a, max_length, max_new);
+        case 5: return attend<64, true, TREE>(kv, a, max_length, max_new);
+        case 6: return attend<128, true, TREE>(kv, a, max_length, max_new);
+        case 7: return attend<192, true, TREE>(kv, a, max_length, max_new);
+        default: return attend<256, true, TREE>(kv, a, max_length, max_new);
     }
+}
+
+extern "C" int siso_kv_attend(siso_kv *kv, int layer, const siso_kv_batch *batch, const void *q, long q_token, long q_head, int heads,
+                              float scale, int window, void *out, float *lse) {
+    return attend<false>(kv, "siso_kv_attend", layer, batch, nullptr, q, q_token, q_head, heads, scale, window, out, lse);
+}
+
+extern "C" int siso_kv_attend_tree(siso_kv *kv, int layer, const siso_kv_batch *batch, const unsigned *mask, const void *q, long q_token, long q_head,
+                                   int heads, float scale, int window, void *out, float *lse) {
+    return attend<true>(kv, "siso_kv_attend_tree", layer, batch, mask, q, q_token, q_head, heads, scale, window, out, lse);
 }

@@ -99,6 +99,8 @@ __device__ __forceinline__ bool kv_is_page(const KvPool &pool, int page) { retur
 __device__ __forceinline__ size_t kv_block_at(const KvPool &pool, int page, int head, int at) {
     return ((size_t)((long)page * pool.kv_heads + head) << pool.shift) * pool.dp + (size_t)(((at & ((1 << pool.shift) - 1)) >> 4) * SISO_KV_BLOCK) * pool.dp;
 }
+// Values in 8 bits: the eight tokens of half h and dimension d, in a block.
+__device__ __forceinline__ size_t kv_v8_at(int dp, int h, int d) { return (((h * (dp >> 6) + (d >> 6)) * 32 + (d & 31)) * 2 + ((d >> 5) & 1)) * 8; }
 __device__ __forceinline__ size_t kv_scale_at(const KvPool &pool, int page, int head, int at) {
     return ((size_t)((long)page * pool.kv_heads + head) << pool.shift) + (at & ((1 << pool.shift) - 1));
 }
@@ -132,3 +134,5 @@ int kv_check_hip(siso_kv *kv, hipError_t e, const char *what);
 KvPool kv_pool(const siso_kv *kv, int layer);
 // Checks a batch for a call that reads the cache (or, layer < 0, does not) and brings it into the kernels' form.
 int kv_batch(siso_kv *kv, const char *call, int layer, const siso_kv_batch *batch, KvBatch *out);
+// The most rows that a sequence of a checked batch can have.
+static inline long kv_max_new(const siso_kv_batch *batch) { return batch->max_new > 0 && batch->max_new < batch->rows ? batch->max_new : batch->rows; }

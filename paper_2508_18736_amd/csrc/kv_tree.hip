@@ -1,0 +1,374 @@
+// Trees of drafted tokens: who is whose ancestor, which path stands, and where its keys and values go (siso_kv_tree,
+// siso_kv_verify_tree, siso_kv_keep).  Their attention is in kv_attend.hip.
+#include <type_traits>
+
+#include "kv_entries.h"
+#include "kv_internal.h"
+
+#define KV_TREE_WORDS (SISO_KV_TREE / 32)
+
+// The row that row i continues: 0 to i - 1, or -1.
+__device__ __forceinline__ int kv_parent(const int *parent, const KvSequence &s, int i) {
+    const int p = parent[s.first + i];
+    return p >= 0 && p < i ? p : -1;
+}
+
+// ---------------------------------------------------------------------------- ancestors
+// One workgroup a sequence, one thread a row.  A row knows the ancestors up to some row; with what that one knows it knows twice as many: eight
+// turns for any tree, one for each doubling of the depth.  Bound by latency: 5 us are a launch and three loads that wait for each other.
+__global__ __launch_bounds__(SISO_KV_TREE) void k_kv_tree(KvBatch batch, const int *parent, unsigned *mask, int *depth) {
+    __shared__ unsigned known[SISO_KV_TREE][KV_TREE_WORDS + 1];  // (a word more: rows lie in other banks)
+    __shared__ int up[SISO_KV_TREE];
+    const KvSequence s = kv_sequence(batch, blockIdx.x);
+    if (s.rows > SISO_KV_TREE || s.rows == 0) return;
+    const int i = threadIdx.x;
+    const bool in = i < s.rows;
+    unsigned mine[KV_TREE_WORDS];
+    int at = in ? kv_parent(parent, s, i) : -1;
+#pragma unroll
+    for (int k = 0; k < KV_TREE_WORDS; ++k) mine[k] = i >> 5 == k ? 1u << (i & 31) : 0u;
+#pragma unroll
+    for (int k = 0; k < KV_TREE_WORDS; ++k) known[i][k] = mine[k];
+    up[i] = at;
+    while (__syncthreads_or(at >= 0)) {
+        if (at >= 0) {
+#pragma unroll
+            for (int k = 0; k < KV_TREE_WORDS; ++k) mine[k] |= known[at][k];
+            at = up[at];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < KV_TREE_WORDS; ++k) known[i][k] = mine[k];
+        up[i] = at;
+    }
+    if (!in) return;
+    u32x4_t *to = (u32x4_t *)(mask + (size_t)(s.first + i) * KV_TREE_WORDS);
+    to[0] = u32x4_t{mine[0], mine[1], mine[2], mine[3]};
+    to[1] = u32x4_t{mine[4], mine[5], mine[6], mine[7]};
+    int count = 0;
+#pragma unroll
+    for (int k = 0; k < KV_TREE_WORDS; ++k) count += __popc(mine[k]);
+    if (depth) depth[s.first + i] = count - 1;
+}
+
+// ---------------------------------------------------------------------------- verification
+struct KvSettle {
+    KvBatch batch;
+    const int *parent, *tokens;
+    int vocab;
+    const void *target;
+    long target_stride;
+    const float *u;
+    int *accepted, *rows, *out;
+};
+#define KV_SETTLE 1024
+
+__device__ __forceinline__ double kv_sum_up(double v, int lane) {  // running sums over a wave
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const double x = __shfl_up(v, off);
+        if (lane >= off) v += x;
+    }
+    return v;
+}
+__device__ __forceinline__ double kv_weight(float x) { return x > 0.f ? (double)x : 0.0; }
+template <class T>
+__device__ __forceinline__ void kv_eight(const T *row, int e, int vocab, float beyond, float (&x)[8]) {
+    if (e + 8 <= vocab) kv_entries8(row + e, x);
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = e + i < vocab ? widen(row[e + i]) : beyond;
+}
+
+// The largest entry of a row, the first of equal ones, -1 without any; the same in every thread.  `sh`: 16 keys.
+template <class T>
+__device__ __forceinline__ int kv_largest(const T *row, int vocab, u64 *sh) {
+    const int t = threadIdx.x;
+    float top = -INFINITY;
+    int at = -1;
+    for (int e = 8 * t; e < vocab; e += 8 * KV_SETTLE) {
+        float x[8];
+        kv_eight(row, e, vocab, __uint_as_float(0x7FC00000u), x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (x[i] > top || (at < 0 && x[i] == top)) {
+                top = x[i];
+                at = e + i;
+            }
+    }
+    u64 key = wave_max(at < 0 ? (u64)0 : pack_key(top + 0.f, (unsigned)at));  // (+ 0: the two zeros are equal)
+    if ((t & 63) == 0) sh[t >> 6] = key;
+    __syncthreads();
+    key = wave_max(sh[t & 15]);
+    __syncthreads();
+    return key ? (int)(0xFFFFFFFFu - (unsigned)key) : -1;
+}
+
+// The first entry at which the running sum of a row's weights exceeds u times their sum; -1 without weight.  Every wave sums a
+// stretch of the row; the one that the bar falls into is then searched by all.  sums: 17 numbers, found: 16 and 16.
+template <class T>
+__device__ __forceinline__ int kv_drawn(const T *row, int vocab, float u, double *sums, int *found) {
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    const int stretch = ((vocab + 16 * 512 - 1) / (16 * 512)) * 512;
+    double sum = 0.0;
+    for (int e = w * stretch + 8 * lane; e < (w + 1) * stretch && e < vocab; e += 512) {
+        float x[8];
+        kv_eight(row, e, vocab, 0.f, x);
+        sum += ((kv_weight(x[0]) + kv_weight(x[1])) + (kv_weight(x[2]) + kv_weight(x[3]))) + ((kv_weight(x[4]) + kv_weight(x[5])) + (kv_weight(x[6]) + kv_weight(x[7])));
+    }
+    sum = wave_fold(sum, [](double a, double b) __attribute__((always_inline)) { return a + b; });
+    if (lane == 0) sums[w] = sum;
+    __syncthreads();
+    const double mine = lane < 16 ? sums[lane & 15] : 0.0, upto = kv_sum_up(mine, lane), total = __shfl(upto, 15);
+    const double bar = (double)fminf(fmaxf(u, 0.f), 0.99999994f) * total;
+    __syncthreads();
+    if (!(total > 0.0)) return -1;
+    // the first stretch with weight in which the bar is passed, or the last one with weight
+    const u64 over = __ballot(mine > 0.0 && upto > bar), some = __ballot(mine > 0.0);
+    const int at = over ? __ffsll((long long)over) - 1 : 63 - __clzll((long long)some);
+    double before = at > 0 ? __shfl(upto, at - 1) : 0.0;
+    int first = 0x7FFFFFFF, last = -1;
+    const int end = (at + 1) * stretch < vocab ? (at + 1) * stretch : vocab;
+    for (int e0 = at * stretch; e0 < end; e0 += 8 * KV_SETTLE) {
+        const int e = e0 + 8 * t;
+        float x[8];
+        double here = 0.0;
+        if (e < end) {
+            kv_eight(row, e, vocab, 0.f, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) here += kv_weight(x[i]);
+        }
+        const double run = kv_sum_up(here, lane);
+        if (lane == 63) sums[w] = run;
+        __syncthreads();
+        double so_far = before + (run - here);
+        for (int i = 0; i < 16; ++i) {
+            if (i < w) so_far += sums[i];
+            before += sums[i];
+        }
+        if (e < end)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double weight = kv_weight(x[i]);
+                so_far += weight;
+                if (weight > 0.0) {
+                    last = e + i;
+                    if (so_far > bar && first == 0x7FFFFFFF) first = e + i;
+                }
+            }
+        __syncthreads();
+    }
+    first = wave_fold(first, [](int a, int b) __attribute__((always_inline)) { return a < b ? a : b; });
+    last = wave_fold(last, [](int a, int b) __attribute__((always_inline)) { return a > b ? a : b; });
+    if (lane == 0) {
+        found[w] = first;
+        found[16 + w] = last;
+    }
+    __syncthreads();
+    first = wave_fold(found[lane & 15], [](int a, int b) __attribute__((always_inline)) { return a < b ? a : b; });
+    last = wave_fold(found[16 + (lane & 15)], [](int a, int b) __attribute__((always_inline)) { return a > b ? a : b; });
+    __syncthreads();
+    return first != 0x7FFFFFFF ? first : last;  // (rounding may leave none: the last one with weight)
+}
+
+// One workgroup a sequence: it goes from row to row and reads those alone.
+template <class T, bool GREEDY>
+__global__ __launch_bounds__(KV_SETTLE) void k_kv_settle(KvSettle a) {
+    __shared__ int parents[SISO_KV_TREE], tokens[SISO_KV_TREE];
+    __shared__ double sums[16];
+    __shared__ u64 keys[16];
+    __shared__ int found[32];
+    const KvSequence s = kv_sequence(a.batch, blockIdx.x);
+    const int t = threadIdx.x, lane = t & 63;
+    if (s.rows > SISO_KV_TREE) return;
+    if (s.rows == 0) {
+        if (t == 0) a.accepted[s.b] = -1;
+        return;
+    }
+    if (t < SISO_KV_TREE) {
+        parents[t] = t < s.rows ? kv_parent(a.parent, s, t) : -1;
+        tokens[t] = t < s.rows ? a.tokens[s.first + t] : -1;
+    }
+    __syncthreads();
+    int row = 0, count = 0;
+    for (;;) {
+        const T *p = (const T *)a.target + (long)(s.first + row) * a.target_stride;
+        int x;
+        if constexpr (GREEDY) x = kv_largest(p, a.vocab, keys);
+        else x = kv_drawn(p, a.vocab, a.u[s.first + row], sums, found);
+        if (t == 0) {
+            a.rows[s.first + count] = row;
+            a.out[s.first + count] = x;
+        }
+        ++count;
+        int child = -1;  // (every wave by itself, and all find the same)
+        for (int i0 = 0; i0 < s.rows && child < 0; i0 += 64) {
+            const u64 fits = __ballot(x >= 0 && parents[i0 + lane] == row && tokens[i0 + lane] == x);
+            if (fits) child = i0 + __ffsll((long long)fits) - 1;
+        }
+        if (child < 0) break;
+        row = child;  // (it lies behind its parent: this ends)
+    }
+    for (int i = count + t; i < s.rows; i += KV_SETTLE) a.rows[s.first + i] = a.out[s.first + i] = -1;
+    if (t == 0) a.accepted[s.b] = count - 1;
+}
+
+// ---------------------------------------------------------------------------- the path that stands
+// One workgroup for a sequence, a layer and a kv head.  Rows move to lower places, and in order: eight at a time are read before they are written, and
+// what is read later lies behind all that has been written.
+#define KV_KEEP_ROWS 8
+template <bool FP8>
+__global__ __launch_bounds__(256) void k_kv_keep(KvPool pool, KvBatch batch, const int *path, long layer_bytes, long layer_scales, int layers, int b0) {
+    constexpr int ES = FP8 ? 1 : 2;
+    using E = typename std::conditional<FP8, unsigned char, bf16_t>::type;
+    const int head = blockIdx.x % pool.kv_heads, layer = blockIdx.x / pool.kv_heads % layers, t = threadIdx.x;
+    const KvSequence s = kv_sequence(batch, b0 + blockIdx.x / pool.kv_heads / layers);
+    char *const pool_k = pool.k + layer * layer_bytes, *const pool_v = pool.v + layer * layer_bytes;
+    float *const scales = FP8 ? (t & 8 ? pool.vs : pool.ks) + layer * layer_scales : nullptr;
+    const int dp = pool.dp, chunks = dp * ES / 16;  // 16-byte chunks of a key
+    const int *const table = batch.pages + (long)s.b * batch.width;
+    __shared__ int count, moves;  // rows of the path, and from which one on they move
+    if (t < 64) {
+        int n = 0, first = 0x7FFFFFFF, before = -1;
+        for (int j0 = 0; j0 < s.rows; j0 += 64) {
+            const int j = j0 + t, p = j < s.rows ? path[s.first + j] : -1;
+            const int up = __shfl_up(p, 1), prior = t ? up : before;
+            before = __shfl(p, 63);
+            const u64 ends = ~__ballot(p >= j && p > prior && p < s.rows);
+            const u64 moved = __ballot(p > j);
+            const int good = ends ? __ffsll((long long)ends) - 1 : 64;
+            if (moved && first == 0x7FFFFFFF) first = j0 + __ffsll((long long)moved) - 1;
+            n = j0 + good;
+            if (good < 64) break;
+        }
+        if (t == 0) {
+            count = n;
+            moves = first;
+        }
+    }
+    __syncthreads();
+    auto place = [&](int row, int &at) {  // of a row of the sequence the page, or -1
+        at = s.start + row;
+        if (at < 0 || at >= batch.most) return -1;
+        const int page = table[at >> pool.shift];
+        if (kv_is_page(pool, page)) return page;
+        if (t == 0 && head == 0) atomicAdd(pool.bad, 1ull);
+        return -1;
+    };
+    for (int j0 = moves; j0 < count; j0 += KV_KEEP_ROWS) {
+        const int here = count - j0 < KV_KEEP_ROWS ? count - j0 : KV_KEEP_ROWS;
+        u32x4_t k = u32x4_t{0, 0, 0, 0};
+        E v[KV_KEEP_ROWS];
+        float scale = 0.f;
+        char *k_to = nullptr;
+        int to[KV_KEEP_ROWS], to_page[KV_KEEP_ROWS];
+        float *scale_to = nullptr;
+        // values: a thread for an element of all rows
+#pragma unroll
+        for (int r = 0; r < KV_KEEP_ROWS; ++r) {
+            to_page[r] = -1;
+            to[r] = 0;
+            v[r] = 0;
+            if (r >= here) continue;
+            int at;
+            const int page = place(path[s.first + j0 + r], at);
+            to_page[r] = place(j0 + r, to[r]);
+            const int key = at & 15;
+            if (page >= 0 && t < dp) {
+                const char *block = pool_v + kv_block_at(pool, page, head, at) * ES;
+                v[r] = FP8 ? ((const E *)block)[kv_v8_at(dp, kv_half(key), t) + kv_slot(key)] : ((const E *)block)[(kv_half(key) * dp + t) * 8 + kv_slot(key)];
+            }
+            // keys: a thread for a chunk of a row
+            if (t / chunks == r) {
+                if (page >= 0) k = *(const u32x4_t *)(pool_k + kv_block_at(pool, page, head, at) * ES + ((t % chunks) * 16 + key) * 16);
+                if (to_page[r] >= 0) k_to = pool_k + kv_block_at(pool, to_page[r], head, to[r]) * ES + ((t % chunks) * 16 + (to[r] & 15)) * 16;
+            }
+            if (FP8 && (t & 7) == r && t < 16) {
+                if (page >= 0) scale = scales[kv_scale_at(pool, page, head, at)];
+                if (to_page[r] >= 0) scale_to = scales + kv_scale_at(pool, to_page[r], head, to[r]);
+            }
+        }
+        __syncthreads();
+        if (k_to) *(u32x4_t *)k_to = k;
+        if (FP8 && scale_to) *scale_to = scale;
+#pragma unroll
+        for (int r = 0; r < KV_KEEP_ROWS; ++r) {
+            if (to_page[r] < 0 || t >= dp) continue;
+            char *block = pool_v + kv_block_at(pool, to_page[r], head, to[r]) * ES;
+            const int key = to[r] & 15;
+            ((E *)block)[FP8 ? kv_v8_at(dp, kv_half(key), t) + kv_slot(key) : (kv_half(key) * dp + t) * 8 + kv_slot(key)] = v[r];
+        }
+        // (no wait: what the next turn reads nobody has written)
+    }
+}
+
+// ---------------------------------------------------------------------------- calls
+static int tree_batch(siso_kv *kv, const char *call, const siso_kv_batch *batch, KvBatch *b) {
+    const int rc = kv_batch(kv, call, -1, batch, b);
+    if (rc != SISO_OK) return rc;
+    if (kv_max_new(batch) > SISO_KV_TREE) return kv_fail(kv, SISO_EINVAL, "%s: trees of %ld rows", call, kv_max_new(batch));
+    return SISO_OK;
+}
+
+extern "C" int siso_kv_tree(siso_kv *kv, const siso_kv_batch *batch, const int *parent, unsigned *out_mask, int *out_depth) {
+    if (!kv) return SISO_EINVAL;
+    KvBatch b;
+    const int rc = tree_batch(kv, "siso_kv_tree", batch, &b);
+    if (rc != SISO_OK) return rc;
+    if (b.n == 0 || b.rows == 0) return SISO_OK;
+    if (!parent || !out_mask || ((uintptr_t)out_mask & 15)) return kv_fail(kv, SISO_EINVAL, "siso_kv_tree: parents and masks must be there, masks 16-byte aligned");
+    hipLaunchKernelGGL(k_kv_tree, dim3(b.n), dim3(SISO_KV_TREE), 0, kv->stream, b, parent, out_mask, out_depth);
+    KV_TRY(kv, hipGetLastError());
+    return SISO_OK;
+}
+
+extern "C" int siso_kv_verify_tree(siso_kv *kv, const siso_kv_batch *batch, const int *parent, const int *tokens, int vocab, int type,
+                                   const void *target, long target_stride, const float *u, int *out_accepted, int *out_rows, int *out_tokens) {
+    if (!kv) return SISO_EINVAL;
+    KvSettle a;
+    const int rc = tree_batch(kv, "siso_kv_verify_tree", batch, &a.batch);
+    if (rc != SISO_OK) return rc;
+    if (vocab < 1 || vocab > (1 << 24)) return kv_fail(kv, SISO_EINVAL, "siso_kv_verify_tree: vocabulary of %d", vocab);
+    if (type != SISO_F32 && type != SISO_BF16) return kv_fail(kv, SISO_EINVAL, "siso_kv_verify_tree: probabilities of type %d", type);
+    if (a.batch.n == 0) return SISO_OK;
+    if (!out_accepted || (a.batch.rows > 0 && (!parent || !tokens || !target || !out_rows || !out_tokens)))
+        return kv_fail(kv, SISO_EINVAL, "siso_kv_verify_tree: parents, tokens, target or outputs are NULL");
+    if ((uintptr_t)target & (type == SISO_F32 ? 3 : 1)) return kv_fail(kv, SISO_EINVAL, "siso_kv_verify_tree: probabilities are not aligned to their type");
+    a.parent = parent;
+    a.tokens = tokens;
+    a.vocab = vocab;
+    a.target = target;
+    a.target_stride = target_stride;
+    a.u = u;
+    a.accepted = out_accepted;
+    a.rows = out_rows;
+    a.out = out_tokens;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.batch.n), dim3(KV_SETTLE), 0, kv->stream, a); };
+    if (type == SISO_F32) u ? go(k_kv_settle<float, false>) : go(k_kv_settle<float, true>);
+    else u ? go(k_kv_settle<bf16_t, false>) : go(k_kv_settle<bf16_t, true>);
+    KV_TRY(kv, hipGetLastError());
+    return SISO_OK;
+}
+
+extern "C" int siso_kv_keep(siso_kv *kv, int layer, const siso_kv_batch *batch, const int *path) {
+    if (!kv) return SISO_EINVAL;
+    if (layer < -1) return kv_fail(kv, SISO_EINVAL, "siso_kv_keep: layer %d", layer);
+    KvBatch b;
+    const int rc = kv_batch(kv, "siso_kv_keep", layer < 0 ? 0 : layer, batch, &b);
+    if (rc != SISO_OK) return rc;
+    if (b.n == 0 || b.rows == 0) return SISO_OK;
+    if (!path) return kv_fail(kv, SISO_EINVAL, "siso_kv_keep: no path");
+    const KvPool pool = kv_pool(kv, layer < 0 ? 0 : layer);
+    const long layers = layer < 0 ? kv->layers : 1;
+    if (layers * kv->kv_heads > 1L << 23) return kv_fail(kv, SISO_EINVAL, "siso_kv_keep: %ld layers of %d kv heads at once", layers, kv->kv_heads);
+    const long each = (1L << 23) / (layers * kv->kv_heads);  // sequences of a launch, which has fewer than 2^32 threads
+    for (long b0 = 0; b0 < b.n; b0 += each) {
+        const dim3 grid((unsigned)((b.n - b0 < each ? b.n - b0 : each) * layers * kv->kv_heads));
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, kv->stream, pool, b, path, (long)kv->layer_bytes, (long)kv->layer_scales, (int)layers, (int)b0);
+        };
+        kv->dtype == SISO_FP8 ? go(k_kv_keep<true>) : go(k_kv_keep<false>);
+        KV_TRY(kv, hipGetLastError());
+    }
+    return SISO_OK;
+}

@@ -78,6 +78,12 @@ SYMBOLS = {
     "siso_kv_read": ([_vp, _it, _vp, _it, _vp, _vp], _it),
     "siso_kv_attend": ([_vp, _it, _vp, _vp, _lg, _lg, _it, _fl, _it, _vp, _vp], _it),
     "siso_kv_verify": ([_vp, _vp, _vp, _it, _it, _vp, _lg, _vp, _lg, _vp, _vp, _vp, _vp], _it),
+    "siso_kv_tree": ([_vp, _vp, _vp, _vp, _vp], _it),
+    "siso_kv_attend_tree": ([_vp, _it, _vp, _vp, _vp, _lg, _lg, _it, _fl, _it, _vp, _vp], _it),
+    "siso_kv_verify_tree": ([_vp, _vp, _vp, _vp, _it, _it, _vp, _lg, _vp, _vp, _vp, _vp], _it),
+    "siso_kv_keep": ([_vp, _it, _vp, _vp], _it),
+    "siso_kv_weigh": ([_vp, _it, _vp, _vp, _lg, _lg, _it, _fl, _it, _vp, _vp, _vp, _fl, _vp, _vp], _it),
+    "siso_kv_evict": ([_vp, _it, _vp, _lg, _lg, _lg, _vp, _vp, _vp, _lg], _it),
     "siso_kv_bad_pages": ([_vp], _lg),
     "siso_kv_last_error": ([_vp], C.c_char_p),
 }
@@ -509,8 +515,27 @@ class KvBatch:
         self._ref = C.addressof(self._c)
 
 
+TREE = 256  # rows of a tree, at most
+
+
+class KvTree:
+    """Trees of drafted tokens, for the rows of a batch (``PagedKV.tree``): ``parent`` int32 [rows], ``mask`` int32 [rows, 8] (who is whose
+    ancestor) and ``depth`` int32 [rows]: a row stands at position length - new rows + depth."""
+
+    def __init__(self, parent: torch.Tensor, mask: torch.Tensor, depth: torch.Tensor):
+        self.parent, self.mask, self.depth = parent, mask, depth
+
+
+class KvWeights:
+    """What the positions of a cache have been weighed with (``PagedKV.weights``): ``mass`` float32 and ``born`` int32 or None,
+    [layers, pages, kv_heads, page_tokens]."""
+
+    def __init__(self, mass: torch.Tensor, born: Optional[torch.Tensor]):
+        self.mass, self.born = mass, born
+
+
 class PagedKV:
-    """The paged key/value cache of a target model, its attention and the verification of drafts (``siso_kv.h``).
+    """The paged key/value cache of a target model, its attention, the verification of drafts, and eviction (``siso_kv.h``).
     Method names follow the C ABI.  Work goes to the stream that was current when the handle was made, or that of
     ``set_stream``; a caller on another stream orders the two."""
 
@@ -580,6 +605,10 @@ class PagedKV:
             raise ValueError(f"{what}: expected a contiguous {list(shape)} {dtype} tensor on {self.device}")
         return t
 
+    def _vec(self, t: Optional[torch.Tensor], dtype: torch.dtype, shape, what: str) -> None:
+        if t is not None and (t.get_device() != self._index or t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
+            raise ValueError(f"{what}: expected a contiguous {list(shape)} {dtype} tensor on {self.device}")
+
     # ---------------------------------------------------------------------- calls
     def batch(self, first: torch.Tensor, length: Optional[torch.Tensor] = None, pages: Optional[torch.Tensor] = None,
               rows: Optional[int] = None, max_new: int = 0, max_length: int = 0) -> KvBatch:
@@ -616,19 +645,24 @@ class PagedKV:
         return out_k, out_v
 
     def attend(self, batch: KvBatch, q: torch.Tensor, layer: int = 0, scale: Optional[float] = None, window: int = 0,
-               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, with_lse: bool = False):
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, with_lse: bool = False, tree: Optional[KvTree] = None):
         """Attention of ``q`` [rows, heads, head_dim] (scale: 1 / sqrt(head_dim) unless given): ``out``, or ``(out, lse)`` if ``lse``
-        is given or asked for."""
+        is given or asked for.  ``tree``: the rows are those of trees, and see the context and their ancestors."""
         q = self._heads(q, batch.rows, None, "q")
         shape, stride = q.shape, q.stride()
         out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else self._out(out, shape, torch.bfloat16, "out")
         if with_lse or lse is not None:
             lse = self._out(lse, shape[:2], torch.float32, "lse")
+        if tree is not None:
+            self._vec(tree.mask, torch.int32, (shape[0], TREE // 32), "tree.mask")
         if self._elsewhere():
-            self._used(q, out, lse, *batch.tensors)
-        rc = _lib.siso_kv_attend(self._h, layer, batch._ref, q.data_ptr(), stride[0], stride[1], shape[1],
-                                 self.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
-                                 None if lse is None else lse.data_ptr())
+            self._used(q, out, lse, None if tree is None else tree.mask, *batch.tensors)
+        rest = (q.data_ptr(), stride[0], stride[1], shape[1], self.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
+                None if lse is None else lse.data_ptr())
+        if tree is None:
+            rc = _lib.siso_kv_attend(self._h, layer, batch._ref, *rest)
+        else:
+            rc = _lib.siso_kv_attend_tree(self._h, layer, batch._ref, tree.mask.data_ptr(), *rest)
         if rc < 0:
             self._check(rc)
         return out if lse is None else (out, lse)
@@ -659,6 +693,102 @@ class PagedKV:
                                         target.data_ptr(), target.stride(0), p(draft), 0 if draft is None else draft.stride(0),
                                         p(u_accept), p(u_sample), out_accepted.data_ptr(), out_tokens.data_ptr()))
         return out_accepted, out_tokens
+
+    def tree(self, batch: KvBatch, parent: torch.Tensor) -> KvTree:
+        """Trees of the batch's rows, at most 256 of a sequence: ``parent`` int32 [rows], of each row the earlier row of its sequence that it
+        continues, or -1."""
+        rows = batch.rows
+        self._vec(parent, torch.int32, (rows,), "parent")
+        mask = torch.empty((rows, TREE // 32), dtype=torch.int32, device=self.device)
+        depth = torch.empty(rows, dtype=torch.int32, device=self.device)
+        if self._elsewhere():
+            self._used(parent, mask, depth, batch.first)
+        self._check(_lib.siso_kv_tree(self._h, batch._ref, parent.data_ptr(), mask.data_ptr(), depth.data_ptr()))
+        return KvTree(parent, mask, depth)
+
+    def verify_tree(self, batch: KvBatch, tree: KvTree, tokens: torch.Tensor, target: torch.Tensor, u: Optional[torch.Tensor] = None,
+                    out_accepted: Optional[torch.Tensor] = None, out_rows: Optional[torch.Tensor] = None,
+                    out_tokens: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """The path of each tree that stands: ``(accepted int32 [n], rows int32 [rows], tokens int32 [rows])``, rows of the path and its
+        tokens with the one that follows, then -1.  ``target`` [rows, vocab], float32 or bfloat16: probabilities with a random number ``u``
+        for each row, or (greedy) logits."""
+        rows = batch.rows
+        self._vec(tree.parent, torch.int32, (rows,), "tree.parent")
+        self._vec(tokens, torch.int32, (rows,), "tokens")
+        self._vec(u, torch.float32, (rows,), "u")
+        if target.get_device() != self._index or target.dtype not in (torch.float32, torch.bfloat16) or target.dim() != 2 or target.shape[0] != rows or \
+                target.stride(1) != 1:
+            raise ValueError(f"target: expected a [{rows}, vocab] float32 or bfloat16 tensor on {self.device}, entries of a row side by side")
+        out_accepted = self._out(out_accepted, (batch.n,), torch.int32, "out_accepted")
+        out_rows, out_tokens = (self._out(t, (rows,), torch.int32, what) for t, what in ((out_rows, "out_rows"), (out_tokens, "out_tokens")))
+        if self._elsewhere():
+            self._used(tree.parent, tokens, target, u, out_accepted, out_rows, out_tokens, *batch.tensors)
+        self._check(_lib.siso_kv_verify_tree(self._h, batch._ref, tree.parent.data_ptr(), tokens.data_ptr(), target.shape[1],
+                                             F32 if target.dtype == torch.float32 else BF16, target.data_ptr(), target.stride(0),
+                                             None if u is None else u.data_ptr(), out_accepted.data_ptr(), out_rows.data_ptr(), out_tokens.data_ptr()))
+        return out_accepted, out_rows, out_tokens
+
+    def keep(self, batch: KvBatch, rows: torch.Tensor, layer: Optional[int] = None) -> None:
+        """The keys and values of the path ``rows`` (int32 [rows], as ``verify_tree`` gives it) move behind the context, in one layer or
+        in all."""
+        self._vec(rows, torch.int32, (batch.rows,), "rows")
+        if self._elsewhere():
+            self._used(rows, *batch.tensors)
+        self._check(_lib.siso_kv_keep(self._h, -1 if layer is None else self._layer(layer), batch._ref, rows.data_ptr()))
+
+    def _layer(self, layer: int) -> int:
+        if not 0 <= layer < self.layers:
+            raise ValueError(f"layer {layer} of {self.layers}")
+        return layer
+
+    def weights(self, mass: Optional[torch.Tensor] = None, born: Optional[torch.Tensor] = None) -> KvWeights:
+        """What ``weigh`` adds up and ``evict`` goes by, [layers, pages, kv_heads, page_tokens]: zeros, or the given tensors (``mass`` alone:
+        slots stand for the positions' ages)."""
+        shape = (self.layers, self.pages, self.kv_heads, self.page_tokens)
+        if mass is None:
+            if born is not None:
+                raise ValueError("born without mass")
+            return KvWeights(torch.zeros(shape, dtype=torch.float32, device=self.device), torch.zeros(shape, dtype=torch.int32, device=self.device))
+        self._vec(mass, torch.float32, shape, "mass")
+        self._vec(born, torch.int32, shape, "born")
+        return KvWeights(mass, born)
+
+    def weigh(self, batch: KvBatch, q: torch.Tensor, lse: torch.Tensor, weights: KvWeights, layer: int = 0, scale: Optional[float] = None,
+              window: int = 0, decay: float = 1.0, fresh: Optional[torch.Tensor] = None, newest: Optional[torch.Tensor] = None) -> None:
+        """The attention weights of ``q`` [rows, heads, head_dim], whose ``lse`` [rows, heads] ``attend`` gave, are added to ``weights``: those of
+        positions before ``fresh`` (int32 [n]; None: before the batch's rows) times ``decay`` before.  ``newest`` int32 [n]: the true position of
+        each sequence's newest token (None: nothing has been evicted)."""
+        q = self._heads(q, batch.rows, None, "q")
+        self._vec(lse, torch.float32, q.shape[:2], "lse")
+        self._vec(fresh, torch.int32, (batch.n,), "fresh")
+        self._vec(newest, torch.int32, (batch.n,), "newest")
+        self._whole(weights)
+        if self._elsewhere():
+            self._used(q, lse, fresh, newest, weights.mass, weights.born, *batch.tensors)
+        p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._check(_lib.siso_kv_weigh(self._h, layer, batch._ref, q.data_ptr(), q.stride(0), q.stride(1), q.shape[1],
+                                       self.head_dim ** -0.5 if scale is None else scale, window, lse.data_ptr(), p(fresh), p(newest), decay,
+                                       weights.mass.data_ptr(), p(weights.born)))
+
+    def _whole(self, weights: KvWeights) -> None:
+        shape = (self.layers, self.pages, self.kv_heads, self.page_tokens)
+        self._vec(weights.mass, torch.float32, shape, "weights.mass")
+        self._vec(weights.born, torch.int32, shape, "weights.born")
+
+    def evict(self, batch: KvBatch, weights: KvWeights, keep: int, recent: int = 0, early: int = 0, layer: Optional[int] = None,
+              to: Optional[torch.Tensor] = None) -> None:
+        """Sequences of more than ``keep`` positions keep so many, in one layer or in all: the newest ``recent``, those before position ``early``, and
+        those with the largest sums.  They then stand at min(length, keep) positions, in their pages, or in the pages ``to`` (int32
+        [n, width]), with what they hold left as it is."""
+        if to is not None and (to.dim() != 2 or to.shape[0] != batch.n):
+            raise ValueError(f"to: expected page numbers of {batch.n} sequences")
+        self._vec(to, torch.int32, None if to is None else to.shape, "to")
+        self._whole(weights)
+        if self._elsewhere():
+            self._used(to, weights.mass, weights.born, *batch.tensors)
+        self._check(_lib.siso_kv_evict(self._h, -1 if layer is None else self._layer(layer), batch._ref, keep, recent, early, weights.mass.data_ptr(),
+                                       None if weights.born is None else weights.born.data_ptr(), None if to is None else to.data_ptr(),
+                                       0 if to is None else to.shape[1]))
 
     def bad_pages(self) -> int:
         return self._check(_lib.siso_kv_bad_pages(self._h))
