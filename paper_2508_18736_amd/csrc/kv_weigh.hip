@@ -35,7 +35,9 @@ struct KvWeigh {
 // Sequences of few rows of work: a workgroup takes a stretch of the positions, KV_STEP at a time, against all rows, which it holds in LDS.
 #define KV_WEIGH_FEW 128
 #define KV_STEP 128
-#define KV_WEIGH_FILL 2048
+// Workgroups: of up to 32 rows of work more than are on the chip at once (64 single tokens over 217,173 positions: 61.6 us a pass, 1,024 62.8, 512 66.2, 8,192
+// 66.2), of more, whose rows every workgroup brings to LDS first, as many (64 rows over 21,608 positions: 20.8 us a pass, 2,048 25.2, 512 22.1).
+#define KV_WEIGH_FILL(work) ((work) > 32 ? 1024 : 2048)
 // Of more rows: a workgroup takes a block of positions, whose keys its waves hold in registers, against a stretch of the rows, which pass through LDS.
 // (two tiles of 32 positions a wave, of more than 128 elements one: the registers hold no more)
 constexpr int kv_subs(int dp) { return dp <= 128 ? 2 : 1; }
@@ -67,8 +69,9 @@ __device__ __forceinline__ bf16x8_t kv_codes_bf16(unsigned a, unsigned b) {  // 
 // rows.  Lengths are known on the device only.
 template <bool FEW>
 struct KvShare {
+    using Count = typename std::conditional<FEW, unsigned, u64>::type;  // (of few rows there are at most 2^24 steps of a sequence, and 2^27 pieces of work)
     int first, rows, length;
-    u64 units;
+    Count units;
     __device__ __forceinline__ void load(const KvWeigh &a, int b, int stretch) {
         first = rows = length = 0;
         units = 0;
@@ -81,23 +84,29 @@ struct KvShare {
         if constexpr (FEW) units = ((unsigned)length + KV_STEP - 1) / KV_STEP;
         else units = (u64)(((unsigned)length + a.block - 1) / (unsigned)a.block) * (((unsigned)(rows * a.group) + stretch - 1) / (unsigned)stretch);
     }
+    // Pieces of work of the sequence, of all heads.
+    __device__ __forceinline__ Count pieces(const KvWeigh &a, unsigned stretch) const {
+        return (FEW ? ((unsigned)units + stretch - 1) / stretch : units) * (unsigned)a.pool.kv_heads;
+    }
 };
 __device__ __forceinline__ u64 kv_wave_sum(u64 v) {
     return wave_fold(v, [](u64 a, u64 b) __attribute__((always_inline)) { return a + b; });
 }
-__device__ __forceinline__ u64 kv_running_sum(u64 v) {
+template <class V>
+__device__ __forceinline__ V kv_running_sum(V v) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-        const u64 x = __shfl_up(v, off);
+        const V x = __shfl_up(v, off);
         if (lane >= off) v += x;
     }
     return v;
 }
+__device__ __forceinline__ u64 kv_divide(u64 a, u64 b) { return (a | b) >> 32 ? a / b : (u64)((unsigned)a / (unsigned)b); }
 // Steps of a stretch: so many that there are not more stretches than workgroups.
 __device__ __forceinline__ unsigned kv_weigh_stretch(const KvWeigh &a, u64 all, u64 sequences) {
     const u64 ends = sequences * a.pool.kv_heads, room = (u64)a.items > ends ? a.items - ends : 0;
-    const u64 s = room ? (all * a.pool.kv_heads + room - 1) / room : 0x7FFFFFFFu;
+    const u64 s = room ? kv_divide(all * a.pool.kv_heads + room - 1, room) : 0x7FFFFFFFu;
     return s < 1 ? 1u : s > 0x7FFFFFFFu ? 0x7FFFFFFFu : (unsigned)s;
 }
 // Rows of work of a stretch: those asked for, or all where the workspace has no room for the sums of so many.
@@ -131,7 +140,7 @@ __global__ __launch_bounds__(1024) void k_kv_weigh_plan(KvWeigh a) {
     __syncthreads();  // (the sums' places are used again)
     for (int c = w; c < chunks; c += 16) {
         share.load(a, 64 * c + lane, (int)stretch);
-        const u64 mine = kv_wave_sum(FEW ? (share.units + stretch - 1) / stretch : share.units);
+        const u64 mine = kv_wave_sum((u64)share.pieces(a, stretch));
         if (lane == 0) before[c] = mine;
     }
     __syncthreads();
@@ -140,7 +149,7 @@ __global__ __launch_bounds__(1024) void k_kv_weigh_plan(KvWeigh a) {
     if (lane == 63) sums[w] = upto;
     __syncthreads();
     for (int i = 0; i < w; ++i) upto += sums[i];
-    if (t < chunks) a.plan->before[t] = (upto - mine) * a.pool.kv_heads;
+    if (t < chunks) a.plan->before[t] = upto - mine;
     if (t == 0) {
         a.plan->all = all;
         a.plan->tiles = sequences;
@@ -156,13 +165,14 @@ struct KvWork {
 // The piece of work `item`, the same in every lane; false: there are not as many.
 template <bool FEW>
 __device__ __forceinline__ bool kv_weigh_find(const KvWeigh &a, u64 item, KvWork &k) {
+    using Count = typename KvShare<FEW>::Count;
     const int lane = threadIdx.x & 63;
     KvShare<FEW> share;
     int chunk = 0;
-    u64 ahead = 0;
+    u64 wanted = item;  // of the 64 sequences
     if (a.batch.n <= 64) {
         share.load(a, lane, a.rows);
-        const u64 all = kv_wave_sum(share.units);
+        const u64 all = a.batch.n == 1 ? __shfl((u64)share.units, 0) : kv_wave_sum((u64)share.units);
         if constexpr (FEW) k.stretch = kv_weigh_stretch(a, all, __popcll(__ballot(share.units > 0)));
         else k.stretch = (unsigned)kv_weigh_rows(a, all);
         if (!FEW && (int)k.stretch != a.rows) share.load(a, lane, (int)k.stretch);
@@ -177,13 +187,12 @@ __device__ __forceinline__ bool kv_weigh_find(const KvWeigh &a, u64 item, KvWork
         }
         chunk = __builtin_amdgcn_readfirstlane(chunk);
         k.stretch = FEW ? kv_weigh_stretch(a, a.plan->all, a.plan->tiles) : (unsigned)kv_weigh_rows(a, a.plan->all);
-        ahead = a.plan->before[chunk];
+        wanted = item - a.plan->before[chunk];
         share.load(a, 64 * chunk + lane, (int)k.stretch);
     }
     k.stretch = __builtin_amdgcn_readfirstlane(k.stretch);
-    const u64 mine = (FEW ? (share.units + k.stretch - 1) / k.stretch : share.units) * a.pool.kv_heads;
-    const u64 upto = ahead + kv_running_sum(mine);
-    const u64 over = __ballot(upto > item);
+    const Count mine = share.pieces(a, k.stretch), upto = a.batch.n == 1 ? mine : kv_running_sum(mine);
+    const u64 over = __ballot((u64)upto > wanted);
     if (over == 0) return false;
     const int at = __ffsll((long long)over) - 1;
     k.s.b = 64 * chunk + at;
@@ -191,9 +200,9 @@ __device__ __forceinline__ bool kv_weigh_find(const KvWeigh &a, u64 item, KvWork
     k.s.rows = __builtin_amdgcn_readlane(share.rows, at);
     k.s.length = __builtin_amdgcn_readlane(share.length, at);
     k.s.start = k.s.length - k.s.rows;
-    const u64 before = upto - mine;
-    const u64 in = item - (((u64)(unsigned)__builtin_amdgcn_readlane((int)(before >> 32), at) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)before, at));
-    k.in = in / (unsigned)a.pool.kv_heads;
+    const u64 before = (u64)(upto - mine);
+    const u64 in = wanted - (((u64)(unsigned)__builtin_amdgcn_readlane((int)(before >> 32), at) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)before, at));
+    k.in = kv_divide(in, (unsigned)a.pool.kv_heads);
     k.head = (int)(in - k.in * (unsigned)a.pool.kv_heads);
     return true;
 }
@@ -434,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_weigh_rows(KvWeigh a) {
         KvWork k;
         if (!kv_weigh_find<false>(a, item, k)) return;
         const unsigned stretches = ((unsigned)(k.s.rows * a.group) + k.stretch - 1) / k.stretch;
-        const unsigned block = (unsigned)(k.in / stretches), piece = (unsigned)(k.in - (u64)block * stretches);
+        const unsigned block = (unsigned)kv_divide(k.in, stretches), piece = (unsigned)(k.in - (u64)block * stretches);
         const int p0 = (int)(block * BLOCK), at = p0 + 32 * SUBS * w;  // the block's positions, this wave's
         bf16x8_t kx[SUBS][NS];
         float scale[SUBS], sum[SUBS] = {};
@@ -664,7 +673,8 @@ static int weigh(siso_kv *kv, KvWeigh &a, long max_length, long max_new) {
     const bool many = max_new * a.group > KV_WEIGH_FEW, few = !many || a.batch.rows < max_new * a.batch.n;  // (otherwise all have max_new rows)
     if (few) {
         const long most = (long)a.batch.n * heads * ((max_length + KV_STEP - 1) / KV_STEP), ends = (long)a.batch.n * heads;
-        a.items = most < KV_WEIGH_FILL + ends ? most : KV_WEIGH_FILL + ends;
+        const long fill = KV_WEIGH_FILL(max_new * a.group);
+        a.items = most < fill + ends ? most : fill + ends;
         a.rows = 1 << 30;
         a.block = 0;
         if (a.batch.n > 64) {
