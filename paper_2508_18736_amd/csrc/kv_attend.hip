@@ -169,6 +169,8 @@ __device__ __forceinline__ void kv_finish(const KvAttend &a, const KvTile &t, in
 #define KV_STRETCHES 1024
 #define KV_LEAST 4  // units of a stretch, at least, one for each wave (one token of 2,001 positions gets 5: the launch has no workgroup for the last part of 4, and the fifth
                     // unit is a second step of one wave)
+#define KV_TREE_WHOLE 20
+#define KV_TREE_ROOT 2.0f
 #define KV_ENOUGH 32 // units that are worth being joined
 #define KV_FULL 256  // workgroups
 #define KV_PLAN_CHUNKS 1024  // 65,535 sequences, 64 each
@@ -207,7 +209,14 @@ struct KvFew {
         if (all_tiles >= (u64)a.items) return 0x7FFFFFFFu;
         const u64 room = a.items - all_tiles < KV_STRETCHES ? a.items - all_tiles : KV_STRETCHES;
         unsigned s = all < KV_FULL * KV_ENOUGH ? (unsigned)all / KV_FULL : KV_ENOUGH;
-        s = s > KV_LEAST ? s : KV_LEAST;
+        if constexpr (TREE) {
+            // A part of a full tile takes about as long to join as a step of its four waves: both together are least for twice the root of a tile's
+            // units, and a tile of few is not cut (16 rows of 32 heads over 8 behind 2,001 positions: 16.2 us, with stretches of 4 20.9; behind 8,000:
+            // 21.2 and 29.8; behind 500: 12.5 and 14.0).
+            const float units = all_tiles ? (float)all / (float)all_tiles : 0.f;
+            const unsigned best = units <= KV_TREE_WHOLE ? KV_TREE_WHOLE : (unsigned)(KV_TREE_ROOT * __builtin_amdgcn_sqrtf(units));
+            s = s > best ? s : best;
+        } else s = s > KV_LEAST ? s : KV_LEAST;
         const u64 most = (all + room - 1) / room;
         return most > 0x7FFFFFFFu ? 0x7FFFFFFFu : s > most ? s : (unsigned)most;
     }
@@ -358,6 +367,7 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
         kv_tile<TREE>(a, tile * 32, 32, t);
         int base;
         Few::range_of(a, t.s.start, t.s.length, base);
+        if constexpr (TREE) stretch = ((unsigned)__builtin_amdgcn_readlane(few.range, at) + count - 1) / count;  // (its pieces alike)
         from = base + KS * (int)(piece * stretch);
         to = piece == count - 1 ? t.hi : from + KS * (int)stretch;
         if (from < (t.lo & ~(KS - 1))) from = t.lo & ~(KS - 1);
@@ -760,6 +770,7 @@ struct KvChunk {
 struct KvPieces {
     long slots, slot0;
     int ways;  // a tile's positions are cut into at most so many pieces
+    int per;   // (trees) of so many blocks at least
 };
 #define KV_PIECE_LEAST 256  // positions
 // A phase of products: operands are read so many products ahead (4: 1% slower, 8: 2%), and the work of the next stages begins behind this one.
@@ -780,6 +791,7 @@ __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces 
     from = t.lo & ~15;  // (no block that nobody sees: its page may be given up)
     blocks = t.hi > from ? (t.hi - from + KEYS - 1) / KEYS : 0;
     per = (blocks + p.ways - 1) / p.ways;
+    if (TREE && per < p.per) per = p.per;
     if (per < KV_PIECE_LEAST / KEYS) per = KV_PIECE_LEAST / KEYS;
     pieces = blocks > 0 ? (blocks + per - 1) / per : 1;
     return true;
@@ -1212,12 +1224,22 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) 
 static int kv_chunk_workgroups(int dp) { return dp == 64 ? 512 : 256; }
 
 template <int DP, bool FP8, bool TREE>
-static int attend_chunks(siso_kv *kv, const KvAttend &a) {
+static int attend_chunks(siso_kv *kv, const KvAttend &a, long max_length, long max_new) {
     using C = KvChunk<DP, FP8>;
     KvPieces p;
+    p.per = 0;
     p.slots = kv_slots_before(a.batch.rows, a.batch.n, a.group, C::ROWS == 256 ? 8 : 7, 1);
     const long tiles = p.slots * kv->kv_heads, room = (long)(SISO_KV_PARTS / KV_CHUNK_PART(C::ROWS, DP));
     long ways = tiles <= kv_chunk_workgroups(DP) / 2 ? kv_chunk_workgroups(DP) / tiles : 1;
+    if constexpr (TREE) {
+        // There are about half as many tiles as there may be (one more for each sequence), or, where all have as many rows, so many; pieces are alike,
+        // whatever the lengths are.
+        const long rows = (long)a.batch.rows * a.group / C::ROWS, same = a.batch.n * ((max_new * a.group + C::ROWS - 1) / C::ROWS);
+        const long likely = (a.batch.rows >= max_new * a.batch.n ? same : rows + (a.batch.n + 1) / 2) * kv->kv_heads;
+        ways = (kv_chunk_workgroups(DP) + likely - 1) / likely;  // (twice as many: 4 trees of 256 rows behind 8,000 positions 185 us, not 164)
+        const long seen = a.window > 0 && a.window + 256L < max_length ? a.window + 256L : max_length, blocks = (seen + C::KEYS - 1) / C::KEYS;
+        p.per = (int)((blocks + ways - 1) / ways);
+    }
     if (ways > room / tiles) ways = room / tiles;
     if (ways > 64) ways = 64;
     if (ways < 1) ways = 1;
@@ -1242,9 +1264,12 @@ static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
     // Which sequences there are is known on the device only: where both kinds can be, both kernels are launched, and each leaves the other's.
     const long seen = a.window > 0 && a.window + 32L < max_length ? a.window + 32L : max_length;
     const long light = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads * seen;
-    a.few = DP <= 128 && light * DP <= (a.batch.rows >= max_new * a.batch.n ? KV_LIGHT : KV_LIGHT_MIXED) ? 1 << 30 : KV_FEW;
+    bool by_few = DP <= 128 && light * DP <= (a.batch.rows >= max_new * a.batch.n ? KV_LIGHT : KV_LIGHT_MIXED);
+    // (trees: whatever the work is, if they do not fill the chunks' tiles; 24 trees of 5 to 64 rows, 4 heads for each: 72 us, by chunks 153)
+    if (TREE) by_few = DP <= 128 && (light * DP <= KV_LIGHT || (long)a.batch.rows * a.group < 192L * a.batch.n);
+    a.few = by_few ? 1 << 30 : KV_FEW;
     if (max_new * a.group > a.few) {
-        const int rc = attend_chunks<DP, FP8, TREE>(kv, a);
+        const int rc = attend_chunks<DP, FP8, TREE>(kv, a, max_length, max_new);
         if (rc != SISO_OK || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
     }
     constexpr int KS = kv_step<DP, FP8>();
