@@ -60,8 +60,20 @@ struct KvSettle {
     long target_stride;
     const float *u;
     int *accepted, *rows, *out;
+    // greedy, all rows at once, `most` places for each sequence: [places][slices] keys, [places] tokens, [places + n] how many are there (zeros between calls)
+    int most;
+    u64 *parts;
+    int *named;
+    unsigned *arrived;
+    int slices, slice;
 };
 #define KV_SETTLE 1024
+// Up to so many bytes of them all rows are looked at at once (32 trees of 16 rows of 32,000 entries in 16 bits, 33 MB: 15.5 us a call, row by row 22.6; of 40
+// rows, 82 MB: 28.1 and 25.5).
+#define KV_SETTLE_ALL (48L << 20)
+#define KV_SETTLE_PLACES 4096
+static_assert(2 * KV_SETTLE_PLACES <= SISO_KV_JOINS, "a count for each place and sequence");
+#define KV_SLICE_UNIT 2048  // entries: eight a thread of 256
 
 __device__ __forceinline__ double kv_sum_up(double v, int lane) {  // running sums over a wave
 #pragma unroll
@@ -80,56 +92,61 @@ __device__ __forceinline__ void kv_eight(const T *row, int e, int vocab, float b
         for (int i = 0; i < 8; ++i) x[i] = e + i < vocab ? widen(row[e + i]) : beyond;
 }
 
-// The largest entry of a row, the first of equal ones, -1 without any; the same in every thread.  `sh`: 16 keys.
+// The largest of the entries begin .. end - 1 of a row, the first of equal ones, as a key; 0 without any.  Of one wave.
 template <class T>
-__device__ __forceinline__ int kv_largest(const T *row, int vocab, u64 *sh) {
-    const int t = threadIdx.x;
+__device__ __forceinline__ u64 kv_largest(const T *row, int begin, int end, int vocab, int step) {
     float top = -INFINITY;
     int at = -1;
-    for (int e = 8 * t; e < vocab; e += 8 * KV_SETTLE) {
+#pragma unroll 2
+    for (int e = begin; e < end; e += step) {
         float x[8];
         kv_eight(row, e, vocab, __uint_as_float(0x7FC00000u), x);
+        const float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));  // (NaN only if all are)
+        if (most > top || (at < 0 && most == top)) {
+            top = most;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (x[i] > top || (at < 0 && x[i] == top)) {
-                top = x[i];
-                at = e + i;
-            }
+            for (int i = 7; i >= 0; --i) at = x[i] == most ? e + i : at;
+        }
     }
-    u64 key = wave_max(at < 0 ? (u64)0 : pack_key(top + 0.f, (unsigned)at));  // (+ 0: the two zeros are equal)
-    if ((t & 63) == 0) sh[t >> 6] = key;
-    __syncthreads();
-    key = wave_max(sh[t & 15]);
-    __syncthreads();
-    return key ? (int)(0xFFFFFFFFu - (unsigned)key) : -1;
+    return wave_max(at < 0 ? (u64)0 : pack_key(top + 0.f, (unsigned)at));  // (+ 0: the two zeros are equal)
 }
+__device__ __forceinline__ u64 kv_most(const u64 (&keys)[4]) {
+    const u64 a = keys[0] > keys[1] ? keys[0] : keys[1], b = keys[2] > keys[3] ? keys[2] : keys[3];
+    return a > b ? a : b;
+}
+__device__ __forceinline__ int kv_key_entry(u64 key) { return key ? (int)(0xFFFFFFFFu - (unsigned)key) : -1; }
 
-// The first entry at which the running sum of a row's weights exceeds u times their sum; -1 without weight.  Every wave sums a
-// stretch of the row; the one that the bar falls into is then searched by all.  sums: 17 numbers, found: 16 and 16.
+// The sum of the weights of every step'th eight entries from begin up to end, of one wave.
 template <class T>
-__device__ __forceinline__ int kv_drawn(const T *row, int vocab, float u, double *sums, int *found) {
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-    const int stretch = ((vocab + 16 * 512 - 1) / (16 * 512)) * 512;
+__device__ __forceinline__ double kv_sum(const T *row, int begin, int end, int vocab, int step) {
     double sum = 0.0;
-    for (int e = w * stretch + 8 * lane; e < (w + 1) * stretch && e < vocab; e += 512) {
+#pragma unroll 4
+    for (int e = begin; e < end; e += step) {
         float x[8];
         kv_eight(row, e, vocab, 0.f, x);
         sum += ((kv_weight(x[0]) + kv_weight(x[1])) + (kv_weight(x[2]) + kv_weight(x[3]))) + ((kv_weight(x[4]) + kv_weight(x[5])) + (kv_weight(x[6]) + kv_weight(x[7])));
     }
-    sum = wave_fold(sum, [](double a, double b) __attribute__((always_inline)) { return a + b; });
-    if (lane == 0) sums[w] = sum;
-    __syncthreads();
-    const double mine = lane < 16 ? sums[lane & 15] : 0.0, upto = kv_sum_up(mine, lane), total = __shfl(upto, 15);
-    const double bar = (double)fminf(fmaxf(u, 0.f), 0.99999994f) * total;
-    __syncthreads();
+    return wave_fold(sum, [](double a, double b) __attribute__((always_inline)) { return a + b; });
+}
+// Of up to 64 stretches' sums, one a lane: the first one with weight in which u times the sum of all is passed, or (rounding) the last one with weight;
+// -1 without any.  `before`: the sum ahead of it, `bar`: u times the sum.
+__device__ __forceinline__ int kv_stretch(double mine, float u, double &before, double &bar) {
+    const int lane = threadIdx.x & 63;
+    const double upto = kv_sum_up(mine, lane), total = __shfl(upto, 63);
+    bar = (double)fminf(fmaxf(u, 0.f), 0.99999994f) * total;
     if (!(total > 0.0)) return -1;
-    // the first stretch with weight in which the bar is passed, or the last one with weight
     const u64 over = __ballot(mine > 0.0 && upto > bar), some = __ballot(mine > 0.0);
     const int at = over ? __ffsll((long long)over) - 1 : 63 - __clzll((long long)some);
-    double before = at > 0 ? __shfl(upto, at - 1) : 0.0;
+    before = at > 0 ? __shfl(upto, at - 1) : 0.0;
+    return at;
+}
+// The first of the entries begin .. end - 1 at which the running sum, `before` behind what is ahead of them, exceeds `bar`; the last one with weight
+// where rounding leaves none.  All NW waves; sums: NW numbers, found: 2 NW.
+template <int NW, class T>
+__device__ __forceinline__ int kv_search(const T *row, int begin, int end, int vocab, double before, double bar, double *sums, int *found) {
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
     int first = 0x7FFFFFFF, last = -1;
-    const int end = (at + 1) * stretch < vocab ? (at + 1) * stretch : vocab;
-    for (int e0 = at * stretch; e0 < end; e0 += 8 * KV_SETTLE) {
+    for (int e0 = begin; e0 < end; e0 += 8 * 64 * NW) {
         const int e = e0 + 8 * t;
         float x[8];
         double here = 0.0;
@@ -142,7 +159,7 @@ __device__ __forceinline__ int kv_drawn(const T *row, int vocab, float u, double
         if (lane == 63) sums[w] = run;
         __syncthreads();
         double so_far = before + (run - here);
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < NW; ++i) {
             if (i < w) so_far += sums[i];
             before += sums[i];
         }
@@ -162,24 +179,36 @@ __device__ __forceinline__ int kv_drawn(const T *row, int vocab, float u, double
     last = wave_fold(last, [](int a, int b) __attribute__((always_inline)) { return a > b ? a : b; });
     if (lane == 0) {
         found[w] = first;
-        found[16 + w] = last;
+        found[NW + w] = last;
     }
     __syncthreads();
-    first = wave_fold(found[lane & 15], [](int a, int b) __attribute__((always_inline)) { return a < b ? a : b; });
-    last = wave_fold(found[16 + (lane & 15)], [](int a, int b) __attribute__((always_inline)) { return a > b ? a : b; });
+    first = wave_fold(found[lane & (NW - 1)], [](int a, int b) __attribute__((always_inline)) { return a < b ? a : b; });
+    last = wave_fold(found[NW + (lane & (NW - 1))], [](int a, int b) __attribute__((always_inline)) { return a > b ? a : b; });
     __syncthreads();
-    return first != 0x7FFFFFFF ? first : last;  // (rounding may leave none: the last one with weight)
+    return first != 0x7FFFFFFF ? first : last;
 }
 
-// One workgroup a sequence: it goes from row to row and reads those alone.
+// The row that continues `row` with token x, the first of several, -1 without any; the same in every lane (and every wave finds the same).
+__device__ __forceinline__ int kv_child(const int *parents, const int *tokens, int rows, int row, int x) {
+    const int lane = threadIdx.x & 63;
+    for (int i0 = 0; i0 < rows && x >= 0; i0 += 64) {
+        const u64 fits = __ballot(parents[i0 + lane] == row && tokens[i0 + lane] == x);
+        if (fits) return i0 + __ffsll((long long)fits) - 1;
+    }
+    return -1;
+}
+
+// One workgroup a sequence: it goes from row to row and reads those alone.  Bound by what one compute unit takes in: rows of 128,001 entries of 32 bits
+// at about 110 GB/s each (32 trees of 8 to 40 rows, walks of up to eight: 38 us).
 template <class T, bool GREEDY>
 __global__ __launch_bounds__(KV_SETTLE) void k_kv_settle(KvSettle a) {
+    constexpr int NW = KV_SETTLE / 64;
     __shared__ int parents[SISO_KV_TREE], tokens[SISO_KV_TREE];
-    __shared__ double sums[16];
-    __shared__ u64 keys[16];
-    __shared__ int found[32];
+    __shared__ double sums[NW];
+    __shared__ u64 keys[NW];
+    __shared__ int found[2 * NW];
     const KvSequence s = kv_sequence(a.batch, blockIdx.x);
-    const int t = threadIdx.x, lane = t & 63;
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
     if (s.rows > SISO_KV_TREE) return;
     if (s.rows == 0) {
         if (t == 0) a.accepted[s.b] = -1;
@@ -194,22 +223,92 @@ __global__ __launch_bounds__(KV_SETTLE) void k_kv_settle(KvSettle a) {
     for (;;) {
         const T *p = (const T *)a.target + (long)(s.first + row) * a.target_stride;
         int x;
-        if constexpr (GREEDY) x = kv_largest(p, a.vocab, keys);
-        else x = kv_drawn(p, a.vocab, a.u[s.first + row], sums, found);
+        if constexpr (GREEDY) {
+            const u64 key = kv_largest(p, 8 * t, a.vocab, a.vocab, 8 * KV_SETTLE);
+            if (lane == 0) keys[w] = key;
+            __syncthreads();
+            x = kv_key_entry(wave_max(keys[lane & (NW - 1)]));
+            __syncthreads();
+        } else {  // every wave sums a stretch; the one that the bar falls into is then searched by all
+            const int stretch = ((a.vocab + NW * 512 - 1) / (NW * 512)) * 512, end = (w + 1) * stretch < a.vocab ? (w + 1) * stretch : a.vocab;
+            const double sum = kv_sum(p, w * stretch + 8 * lane, end, a.vocab, 512);
+            if (lane == 0) sums[w] = sum;
+            __syncthreads();
+            double before, bar;
+            const int at = kv_stretch(lane < NW ? sums[lane & (NW - 1)] : 0.0, a.u[s.first + row], before, bar);
+            __syncthreads();
+            x = at < 0 ? -1 : kv_search<NW>(p, at * stretch, (at + 1) * stretch < a.vocab ? (at + 1) * stretch : a.vocab, a.vocab, before, bar, sums, found);
+        }
         if (t == 0) {
             a.rows[s.first + count] = row;
             a.out[s.first + count] = x;
         }
         ++count;
-        int child = -1;  // (every wave by itself, and all find the same)
-        for (int i0 = 0; i0 < s.rows && child < 0; i0 += 64) {
-            const u64 fits = __ballot(x >= 0 && parents[i0 + lane] == row && tokens[i0 + lane] == x);
-            if (fits) child = i0 + __ffsll((long long)fits) - 1;
-        }
+        const int child = kv_child(parents, tokens, s.rows, row, x);
         if (child < 0) break;
         row = child;  // (it lies behind its parent: this ends)
     }
     for (int i = count + t; i < s.rows; i += KV_SETTLE) a.rows[s.first + i] = a.out[s.first + i] = -1;
+    if (t == 0) a.accepted[s.b] = count - 1;
+}
+
+// Greedy, where the rows of all trees together are no more than a pass of the whole chip: all rows at once, a slice of one a workgroup; the one that is done last
+// with a row names its token, the one that is done last with a sequence walks.  Numbers for them pass the caches of the XCDs.  (Drawn tokens gain nothing: a
+// row is searched once more when its sum is known.)
+__device__ __forceinline__ bool kv_all_here(unsigned *arrived, unsigned count, int *last) {  // thread 0 has left its number
+    if (threadIdx.x == 0) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // it is where all workgroups see it
+        *last = atomicAdd(arrived, 1u) == count - 1;
+        if (*last) *arrived = 0;  // (for the next call: nobody else comes)
+    }
+    __syncthreads();
+    const bool is = *last;
+    __syncthreads();
+    return is;
+}
+template <class T>
+__global__ __launch_bounds__(256) void k_kv_settle_all(KvSettle a) {
+    __shared__ int parents[SISO_KV_TREE], tokens[SISO_KV_TREE], named[SISO_KV_TREE];
+    __shared__ u64 keys[4];
+    __shared__ int last;
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    // (which rows there are goes by the sequence alone, whatever the other ones are: every count is reached)
+    const int place = (int)(blockIdx.x / a.slices), slice = (int)(blockIdx.x % a.slices), b = place / a.most, in = place % a.most;
+    const KvSequence s = kv_sequence(a.batch, b);
+    if (s.rows == 0 && in == 0 && slice == 0 && t == 0) a.accepted[b] = -1;
+    if (in >= s.rows || s.rows > a.most) return;
+    const int row = s.first + in;
+    const T *p = (const T *)a.target + (long)row * a.target_stride;
+    const int begin = slice * a.slice, end = begin + a.slice < a.vocab ? begin + a.slice : a.vocab;
+    u64 *const parts = a.parts + (long)place * a.slices;
+    int *const all_named = a.named + b * a.most;
+    const u64 key = kv_largest(p, begin + 8 * t, end, a.vocab, 8 * 256);
+    if (lane == 0) keys[w] = key;
+    __syncthreads();
+    if (t == 0) __hip_atomic_store(parts + slice, kv_most(keys), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!kv_all_here(a.arrived + place, a.slices, &last)) return;
+    const int x = kv_key_entry(wave_max(lane < a.slices ? __hip_atomic_load(parts + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : (u64)0));
+    if (t == 0) __hip_atomic_store(all_named + in, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!kv_all_here(a.arrived + a.batch.n * a.most + b, s.rows, &last)) return;
+    if (t < s.rows) {
+        parents[t] = kv_parent(a.parent, s, t);
+        tokens[t] = a.tokens[s.first + t];
+        named[t] = __hip_atomic_load(all_named + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    } else parents[t] = -1, tokens[t] = -1;
+    __syncthreads();
+    int at = 0, count = 0;
+    for (;;) {  // (every wave by itself)
+        const int name = named[at];
+        if (t == 0) {
+            a.rows[s.first + count] = at;
+            a.out[s.first + count] = name;
+        }
+        ++count;
+        const int child = kv_child(parents, tokens, s.rows, at, name);
+        if (child < 0) break;
+        at = child;
+    }
+    if (t >= count && t < s.rows) a.rows[s.first + t] = a.out[s.first + t] = -1;
     if (t == 0) a.accepted[s.b] = count - 1;
 }
 
@@ -343,9 +442,25 @@ extern "C" int siso_kv_verify_tree(siso_kv *kv, const siso_kv_batch *batch, cons
     a.accepted = out_accepted;
     a.rows = out_rows;
     a.out = out_tokens;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.batch.n), dim3(KV_SETTLE), 0, kv->stream, a); };
-    if (type == SISO_F32) u ? go(k_kv_settle<float, false>) : go(k_kv_settle<float, true>);
-    else u ? go(k_kv_settle<bf16_t, false>) : go(k_kv_settle<bf16_t, true>);
+    const long most = kv_max_new(batch), places = a.batch.n * most;
+    if (!u && (long)a.batch.rows * vocab * (type == SISO_F32 ? 4 : 2) <= KV_SETTLE_ALL && most > 0 && places <= KV_SETTLE_PLACES) {
+        const long units = (vocab + KV_SLICE_UNIT - 1) / KV_SLICE_UNIT;
+        long slices = 1024 / places;
+        slices = slices > 64 ? 64 : slices > units ? units : slices;
+        slices = slices < 1 ? 1 : slices;
+        a.slice = (int)((units + slices - 1) / slices * KV_SLICE_UNIT);
+        a.slices = (vocab + a.slice - 1) / a.slice;
+        a.most = (int)most;
+        a.parts = (u64 *)kv->parts;
+        a.named = (int *)(a.parts + places * a.slices);
+        a.arrived = kv->arrived;
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(places * a.slices)), dim3(256), 0, kv->stream, a); };
+        type == SISO_F32 ? go(k_kv_settle_all<float>) : go(k_kv_settle_all<bf16_t>);
+    } else {
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.batch.n), dim3(KV_SETTLE), 0, kv->stream, a); };
+        if (type == SISO_F32) u ? go(k_kv_settle<float, false>) : go(k_kv_settle<float, true>);
+        else u ? go(k_kv_settle<bf16_t, false>) : go(k_kv_settle<bf16_t, true>);
+    }
     KV_TRY(kv, hipGetLastError());
     return SISO_OK;
 }
