@@ -41,70 +41,130 @@ __device__ __forceinline__ long kv_spot(const KvPool &pool, const int *table, in
     const int page = table[at >> pool.shift];
     return kv_is_page(pool, page) ? (long)kv_scale_at(pool, page, head, at) : -1;
 }
-// Numbers that are ordered as the masses are; what has none is less than all else.
+// Numbers that are ordered as the masses are; NaN is less than all else (and 0, of positions without a page, is less than that).
 __device__ __forceinline__ unsigned kv_order(float mass) {
     const unsigned x = __float_as_uint(mass + 0.f);  // (the two zeros are equal)
-    return mass != mass ? 0u : x >> 31 ? ~x : x | 0x80000000u;
+    return mass != mass ? 1u : x >> 31 ? ~x : x | 0x80000000u;
 }
 
-#define KV_CHOOSE 1024
 #define KV_DIGIT 2048
 
 // ---------------------------------------------------------------------------- which positions stay
-// One workgroup a unit.  The `keep`-th largest number is found digit by digit (11, 11 and 10 bits), from counts of each digit's
-// values.  Each wave then goes over a stretch of the slots, in order.
-__global__ __launch_bounds__(KV_CHOOSE) void k_kv_choose(KvEvict a) {
+#define KV_CHOOSE_ROOM 32768  // words of LDS: two for each position (its number and its age), or one; of more positions both are read from memory whenever they are asked for
+#define KV_CHOOSE_FEW 2048    // positions, up to which a workgroup has 256 threads, beyond 1,024
+// One workgroup a unit.  Its positions' numbers are brought to LDS once; the `keep`-th largest is found digit by digit (11, 11 and 10 bits), from counts of
+// each digit's values.  Each wave then goes over a stretch of the slots, in order: ranks are counts of ballots, so that nothing depends on scheduling.
+// Bound by latency: about ten passes over LDS with a barrier each behind two dependent loads (page, then mass and born).
+template <int NT>
+__global__ __launch_bounds__(NT) void k_kv_choose(KvEvict a, int room) {
+    extern __shared__ unsigned numbers[];
     __shared__ unsigned counts[KV_DIGIT];
-    __shared__ unsigned waves[3][16];
-    __shared__ int newest_of[16];
-    __shared__ unsigned digit, above;
-    const long unit = a.unit0 + blockIdx.x;
-    const KvUnit u = kv_unit(a, unit);
+    constexpr int NW = NT / 64, EACH = KV_DIGIT / NT;
+    __shared__ unsigned waves[3][NW];
+    __shared__ int newest_of[NW];
+    __shared__ unsigned digit, above, same_digit;
+    const KvUnit u = kv_unit(a, a.unit0 + blockIdx.x);
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), length = u.s.length, keep = a.keep;
     int *const from = a.from + (long)blockIdx.x * keep, *const list = a.list + (long)blockIdx.x * keep;
     float *const mass = a.mass + u.layer * a.layer_scales;
     int *const born = a.born ? a.born + u.layer * a.layer_scales : nullptr;
     const int *const table = a.batch.pages + (long)u.s.b * a.batch.width, *const to = a.to ? a.to + (long)u.s.b * a.to_width : nullptr;
     const int to_most = a.to_width > (SISO_KV_MOST >> a.pool.shift) ? (int)SISO_KV_MOST : (int)(a.to_width << a.pool.shift);
-    const bool all = length <= keep;
-    if (all && !to) {
-        return;
-    }
-    int newest = 0;
-    if (!all && born) {
-        newest = -0x7FFFFFFF - 1;
-        for (int i = t; i < length; i += KV_CHOOSE) {
-            const long at = kv_spot(a.pool, table, u.head, i);
-            if (at >= 0 && born[at] > newest) newest = born[at];
+    const bool all = length <= keep, cached = length <= room;
+    if (all && !to) return;
+    // Numbers: MANY positions of a thread at a time.
+    constexpr int MANY = 8;
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        for (int i0 = t; i0 < length; i0 += MANY * NT) {
+            long at[MANY];
+#pragma unroll
+            for (int k = 0; k < MANY; ++k) {
+                const int i = i0 + k * NT;
+                at[k] = kv_spot(a.pool, table, u.head, i < length ? i : i0);
+            }
+            f(i0, at);
         }
+    };
+    const bool both = born && 2L * length <= room;  // ages, too, are in LDS
+    constexpr int NEVER = -0x7FFFFFFF - 1;
+    int newest = length - 1;
+    if (!all && born) {
+        newest = NEVER;
+        each([&](int i0, const long (&at)[MANY]) __attribute__((always_inline)) {
+            int when[MANY];
+            float weight[MANY];
+#pragma unroll
+            for (int k = 0; k < MANY; ++k) {
+                when[k] = at[k] >= 0 ? born[at[k]] : NEVER;
+                weight[k] = both && at[k] >= 0 ? mass[at[k]] : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < MANY; ++k) newest = when[k] > newest ? when[k] : newest;
+            if (both)
+#pragma unroll
+                for (int k = 0; k < MANY; ++k)
+                    if (i0 + k * NT < length) {
+                        numbers[i0 + k * NT] = at[k] >= 0 ? kv_order(weight[k]) : 0u;
+                        numbers[length + i0 + k * NT] = (unsigned)when[k];
+                    }
+        });
         newest = wave_fold(newest, [](int x, int y) __attribute__((always_inline)) { return x > y ? x : y; });
         if (lane == 0) newest_of[w] = newest;
         __syncthreads();
-        newest = wave_fold(newest_of[lane & 15], [](int x, int y) __attribute__((always_inline)) { return x > y ? x : y; });
-    } else newest = length - 1;
+        newest = wave_fold(newest_of[lane & (NW - 1)], [](int x, int y) __attribute__((always_inline)) { return x > y ? x : y; });
+    }
     const long recent_from = (long)newest - a.recent;  // above that
+    auto safe = [&](int when) { return when > recent_from || when < a.early; };
+    auto number_of = [&](long at, int when, float weight) { return at < 0 ? 0u : safe(when) ? 0xFFFFFFFFu : kv_order(weight); };
+    if (!all && both) {  // (a thread's own)
+#pragma unroll 4
+        for (int i = t; i < length; i += NT)
+            if (numbers[i] != 0 && safe((int)numbers[length + i])) numbers[i] = 0xFFFFFFFFu;
+    } else if (!all && cached)
+        each([&](int i0, const long (&at)[MANY]) __attribute__((always_inline)) {
+            int when[MANY];
+            float weight[MANY];
+#pragma unroll
+            for (int k = 0; k < MANY; ++k) {
+                weight[k] = at[k] >= 0 ? mass[at[k]] : 0.f;
+                when[k] = !born ? i0 + k * NT : at[k] >= 0 ? born[at[k]] : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < MANY; ++k)
+                if (i0 + k * NT < length) numbers[i0 + k * NT] = number_of(at[k], when[k], weight[k]);
+        });
     auto number = [&](int i) -> unsigned {
+        if (cached) return numbers[i];
         const long at = kv_spot(a.pool, table, u.head, i);
-        if (at < 0) return 0u;
-        const int when = born ? born[at] : i;
-        return when > recent_from || when < a.early ? 0xFFFFFFFFu : kv_order(mass[at]);
+        return number_of(at, !born ? i : at >= 0 ? born[at] : 0, at >= 0 ? mass[at] : 0.f);
     };
     unsigned bar = 0;  // what is above it stays, and of what is equal the first `ties`
     int ties = 0;
+    bool every = true;  // all that is equal
     if (!all) {
         unsigned left = keep;  // of the numbers that have the digits found so far, so many stay
         for (int turn = 0; turn < 3; ++turn) {
             const int shift = turn == 0 ? 21 : turn == 1 ? 10 : 0, bits = turn == 2 ? 10 : 11;
-            for (int i = t; i < KV_DIGIT; i += KV_CHOOSE) counts[i] = 0;
+            for (int i = t; i < KV_DIGIT; i += NT) counts[i] = 0;
             __syncthreads();
-            for (int i = t; i < length; i += KV_CHOOSE) {
-                const unsigned x = number(i);
-                if (turn == 0 || (x >> (shift + bits)) == (bar >> (shift + bits))) atomicAdd(&counts[(x >> shift) & ((1u << bits) - 1)], 1u);
+            for (int i0 = t; i0 < length; i0 += 4 * NT) {
+                unsigned x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = i0 + k * NT < length ? number(i0 + k * NT) : 0u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i0 + k * NT < length && (turn == 0 || (x[k] >> (shift + bits)) == (bar >> (shift + bits))))
+                        atomicAdd(&counts[(x[k] >> shift) & ((1u << bits) - 1)], 1u);
             }
             __syncthreads();
-            // from the top: thread t has digits 2047 - 2 t and 2046 - 2 t
-            const unsigned c0 = counts[KV_DIGIT - 1 - 2 * t], c1 = counts[KV_DIGIT - 2 - 2 * t];
-            unsigned upto = c0 + c1;
+            // from the top: thread t has EACH digits from KV_DIGIT - 1 - EACH t down
+            unsigned c[EACH], mine = 0;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                c[k] = counts[KV_DIGIT - 1 - EACH * t - k];
+                mine += c[k];
+            }
+            unsigned upto = mine;
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
                 const unsigned x = __shfl_up(upto, off);
@@ -113,155 +173,220 @@ __global__ __launch_bounds__(KV_CHOOSE) void k_kv_choose(KvEvict a) {
             if (lane == 63) waves[0][w] = upto;
             __syncthreads();
             for (int i = 0; i < w; ++i) upto += waves[0][i];
-            const unsigned before = upto - c0 - c1;
-            if (before < left && upto >= left) {
-                const bool second = before + c0 < left;
-                digit = second ? KV_DIGIT - 2 - 2 * t : KV_DIGIT - 1 - 2 * t;
-                above = second ? before + c0 : before;
+            if (upto - mine < left && upto >= left) {
+                unsigned ahead = upto - mine;
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) {
+                    if (ahead < left && ahead + c[k] >= left) {
+                        digit = KV_DIGIT - 1 - EACH * t - k;
+                        above = ahead;
+                        same_digit = c[k];
+                    }
+                    ahead += c[k];
+                }
             }
             __syncthreads();
             bar |= digit << shift;
             left -= above;
+            every = same_digit == left;
+            if (every) break;  // (with whatever digits follow)
         }
         ties = (int)left;
     }
     // a wave's slots, 64 at a time
-    const int stretch = ((length + KV_CHOOSE - 1) / KV_CHOOSE) * 64, begin = w * stretch;
+    const int stretch = ((length + NT - 1) / NT) * 64, begin = w * stretch;
     const int end = begin + stretch < length ? begin + stretch : length;
-    unsigned equal = 0;
-    if (!all)
-        for (int i0 = begin; i0 < end; i0 += 64) equal += __popcll(__ballot(i0 + lane < end && number(i0 + lane) == bar));
-    if (lane == 0) waves[0][w] = equal;
-    __syncthreads();
-    unsigned equal_before = 0;
-    for (int i = 0; i < w; ++i) equal_before += waves[0][i];
     const u64 below = ((u64)1 << lane) - 1;
-    auto stays = [&](int i, unsigned &equals) {  // of the wave's next 64 slots
-        const unsigned x = i < end ? number(i) : 0u;
-        const u64 same = __ballot(i < end && x == bar);
-        const bool yes = all ? i < end : i < end && (x > bar || (x == bar && equals + __popcll(same & below) < (unsigned)ties));
-        equals += __popcll(same);
-        return yes;
+    auto first_bits = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : ((u64)1 << n) - 1; };
+    constexpr int AHEAD = 4;  // 64 slots, so many times
+    auto in_order = [&](auto f) __attribute__((always_inline)) {
+        for (int i0 = begin; i0 < end; i0 += 64 * AHEAD) {
+            unsigned x[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) x[k] = !all && i0 + 64 * k + lane < end ? number(i0 + 64 * k + lane) : 0u;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) f(i0 + 64 * k, x[k]);
+        }
     };
-    unsigned holes = 0, movers = 0, equals = equal_before;
-    for (int i0 = begin; i0 < end; i0 += 64) {
-        const int i = i0 + lane;
-        const bool yes = stays(i, equals);
-        holes += __popcll(__ballot(i < keep && i < end && !yes));
-        movers += __popcll(__ballot(i >= keep && yes));
+    unsigned equal_before = 0;
+    if (!every) {
+        unsigned equal = 0;
+        in_order([&](int base, unsigned x) __attribute__((always_inline)) { equal += __popcll(__ballot(x == bar) & first_bits(end - base)); });
+        if (lane == 0) waves[0][w] = equal;
+        __syncthreads();
+        for (int i = 0; i < w; ++i) equal_before += waves[0][i];
     }
+    unsigned equals = equal_before, hole = 0, mover = 0;
+    auto stays = [&](int base, unsigned x) __attribute__((always_inline)) {  // of the wave's next 64 slots
+        const u64 in = first_bits(end - base);
+        if (every) return (all ? ~0ull : __ballot(x >= bar)) & in;
+        const u64 same = __ballot(x == bar) & in;
+        const bool early = (same >> lane & 1) && equals + __popcll(same & below) < (unsigned)ties;
+        equals += __popcll(same);
+        return __ballot(x > bar || early) & in;
+    };
+    in_order([&](int base, unsigned x) __attribute__((always_inline)) {
+        const u64 yes = stays(base, x), low = first_bits(keep - base);
+        hole += __popcll(low & first_bits(end - base) & ~yes);
+        mover += __popcll(yes & ~low);
+    });
     if (lane == 0) {
-        waves[1][w] = holes;
-        waves[2][w] = movers;
+        waves[1][w] = hole;
+        waves[2][w] = mover;
     }
     __syncthreads();
-    unsigned hole = 0, mover = 0;
+    hole = mover = 0;
     for (int i = 0; i < w; ++i) {
         hole += waves[1][i];
         mover += waves[2][i];
     }
     equals = equal_before;
-    for (int i0 = begin; i0 < end; i0 += 64) {
-        const int i = i0 + lane;
-        const bool yes = stays(i, equals), empty = i < keep && i < end && !yes, moves = i >= keep && yes;
-        const u64 empties = __ballot(empty), movings = __ballot(moves);
-        if (i < keep && i < end) from[i] = empty ? -2 - (int)(hole + __popcll(empties & below)) : to ? i : -1;
-        if (moves) list[mover + __popcll(movings & below)] = i;
+    in_order([&](int base, unsigned x) __attribute__((always_inline)) {
+        const u64 yes = stays(base, x), low = first_bits(keep - base), empties = low & first_bits(end - base) & ~yes, movings = yes & ~low;
+        const int i = base + lane;
+        if (i < keep && i < end) from[i] = empties >> lane & 1 ? -2 - (int)(hole + __popcll(empties & below)) : to ? i : -1;
+        if (movings >> lane & 1) list[mover + __popcll(movings & below)] = i;
         hole += __popcll(empties);
         mover += __popcll(movings);
-    }
+    });
     __syncthreads();  // (what the workgroup has written to memory its own threads see)
-    for (int i = t; i < u.stay; i += KV_CHOOSE) {
-        int of = from[i];
-        if (of <= -2) {
-            of = list[-2 - of];
-            from[i] = of;
+    constexpr int MOVES = 4;
+    for (int i0 = t; i0 < u.stay; i0 += MOVES * NT) {
+        int of[MOVES];
+#pragma unroll
+        for (int k = 0; k < MOVES; ++k) of[k] = i0 + k * NT < u.stay ? from[i0 + k * NT] : -1;
+#pragma unroll
+        for (int k = 0; k < MOVES; ++k)
+            if (of[k] <= -2) {
+                of[k] = list[-2 - of[k]];
+                from[i0 + k * NT] = of[k];
+            }
+        long at[MOVES], spot[MOVES];
+        float weight[MOVES];
+        int when[MOVES];
+#pragma unroll
+        for (int k = 0; k < MOVES; ++k) {
+            const int i = i0 + k * NT;
+            at[k] = of[k] >= 0 ? kv_spot(a.pool, table, u.head, of[k]) : -1;
+            spot[k] = of[k] < 0 || (to && i >= to_most) ? -1 : kv_spot(a.pool, to ? to : table, u.head, i);
         }
-        if (of < 0) continue;
-        const long at = kv_spot(a.pool, table, u.head, of), spot = to ? (i < to_most ? kv_spot(a.pool, to, u.head, i) : -1) : kv_spot(a.pool, table, u.head, i);
-        if (spot < 0) continue;
-        mass[spot] = at >= 0 ? mass[at] : 0.f;
-        if (born) born[spot] = at >= 0 ? born[at] : 0;
+#pragma unroll
+        for (int k = 0; k < MOVES; ++k) {
+            weight[k] = at[k] >= 0 ? mass[at[k]] : 0.f;
+            when[k] = born && at[k] >= 0 ? born[at[k]] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < MOVES; ++k)
+            if (spot[k] >= 0) {
+                mass[spot[k]] = weight[k];
+                if (born) born[spot[k]] = when[k];
+            }
     }
 }
 
 // ---------------------------------------------------------------------------- what moves
-// One workgroup for a block of 16 slots of a unit: keys a thread for a chunk of 16 bytes, values a thread for a dimension of a half's eight tokens.
-// What is read in place lies behind all that is written.
-template <bool FP8>
+// One wave for a block of 16 slots of a unit.  A lane has every fourth chunk of one slot's key, and of every 64th dimension (in the order in which they lie) the
+// eight tokens of each half, from as many places, whose addresses are the wave's.  What is read in place lies behind all that is written.
+// Bound by lines that are read for a part: of a token's value every eighth element of its half's lines is its own (10,240 positions of 8 heads out of
+// 25,683 in 8 bits).
+template <int DP, bool FP8>
 __global__ __launch_bounds__(256) void k_kv_move(KvEvict a, int blocks) {
-    constexpr int ES = FP8 ? 1 : 2;
+    constexpr int ES = FP8 ? 1 : 2, CHUNKS = DP * ES / 16, NC = CHUNKS * 16 / 64;
     using E = typename std::conditional<FP8, byte_t, bf16_t>::type;
     using Eight = typename std::conditional<FP8, uint2, u32x4_t>::type;
-    __shared__ int from[16], page_of[16];
-    const long unit = a.unit0 + blockIdx.x / blocks;
-    const int block = (int)(blockIdx.x % blocks), t = threadIdx.x;
-    const KvUnit u = kv_unit(a, unit);
-    const int at = 16 * block;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), four = (blocks + 3) / 4;
+    const long in_launch = blockIdx.x / four;
+    const int at = 16 * ((int)(blockIdx.x % four) * 4 + w);
+    const KvUnit u = kv_unit(a, a.unit0 + in_launch);
     if (at >= u.stay || (!a.to && u.s.length <= a.keep)) return;
     const int *const table = a.batch.pages + (long)u.s.b * a.batch.width;
-    if (t < 16) {
-        const int of = at + t < u.stay ? a.from[(blockIdx.x / blocks) * (long)a.keep + at + t] : -1;
-        from[t] = of;
-        int page = of >= 0 ? table[of >> a.pool.shift] : -1;
-        if (of >= 0 && !kv_is_page(a.pool, page)) {
-            page = -1;
-            if (u.head == 0) atomicAdd(a.pool.bad, 1ull);
-        }
-        page_of[t] = page;
+    const int key = lane & 15;
+    const int of = at + key < u.stay ? a.from[in_launch * a.keep + at + key] : -1;  // (the same in every 16 lanes)
+    if (__ballot(of >= 0) == 0) return;
+    int of_page = of >= 0 ? table[of >> a.pool.shift] : -1;
+    if (a.to && (at >> a.pool.shift) >= a.to_width) return;
+    const int page = a.to ? a.to[(long)u.s.b * a.to_width + (at >> a.pool.shift)] : table[at >> a.pool.shift];
+    if (of >= 0 && !kv_is_page(a.pool, of_page)) {
+        of_page = -1;
+        if (u.head == 0 && lane < 16) atomicAdd(a.pool.bad, 1ull);
     }
-    __syncthreads();
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) any = any || from[i] >= 0;
-    if (!any) return;
-    int page;
-    if (a.to) {
-        if ((at >> a.pool.shift) >= a.to_width) return;
-        page = a.to[(long)u.s.b * a.to_width + (at >> a.pool.shift)];
-    } else page = table[at >> a.pool.shift];
     if (!kv_is_page(a.pool, page)) {
-        if (t == 0 && u.head == 0) atomicAdd(a.pool.bad, 1ull);
+        if (lane == 0 && u.head == 0) atomicAdd(a.pool.bad, 1ull);
         return;
     }
-    const int dp = a.pool.dp, chunks = dp * ES / 16;
     char *const pool_k = a.pool.k + u.layer * a.layer_bytes, *const pool_v = a.pool.v + u.layer * a.layer_bytes;
-    char *const kb = pool_k + kv_block_at(a.pool, page, u.head, at) * ES, *const vb = pool_v + kv_block_at(a.pool, page, u.head, at) * ES;
-    for (int i = t; i < 16 * chunks; i += 256) {
-        const int key = i & 15, c = i >> 4, of = from[key];
-        if (of < 0) continue;
-        u32x4_t x = u32x4_t{0, 0, 0, 0};
-        if (page_of[key] >= 0) x = *(const u32x4_t *)(pool_k + kv_block_at(a.pool, page_of[key], u.head, of) * ES + (c * 16 + (of & 15)) * 16);
-        *(u32x4_t *)(kb + (c * 16 + key) * 16) = x;
+    const size_t to_block = kv_block_at(a.pool, page, u.head, at) * ES;
+    u32x4_t k[NC];
+    {
+        const char *from_k = pool_k + kv_block_at(a.pool, of_page >= 0 ? of_page : 0, u.head, of >= 0 ? of : 0) * ES + (of & 15) * 16;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            k[c] = u32x4_t{0, 0, 0, 0};
+            if (of_page >= 0) k[c] = *(const u32x4_t *)(from_k + ((lane >> 4) + 4 * c) * 256);
+        }
     }
-    for (int i = t; i < 2 * dp; i += 256) {
-        const int h = i >= dp, d = i - h * dp;
-        auto eight_at = [&](int half) { return FP8 ? kv_v8_at(dp, half, d) : (size_t)(half * dp + d) * 8; };
-        E x[8];
+    const bool full = (__ballot(of_page >= 0) & 0xFFFFu) == 0xFFFFu;  // all 16 come from pages: loads that wait for nothing but their addresses
+    float scale = 0.f;
+    float *const scales = (lane < 16 ? a.pool.ks : a.pool.vs) + u.layer * a.layer_scales;
+    if (FP8 && lane < 32 && of_page >= 0) scale = scales[kv_scale_at(a.pool, of_page, u.head, of)];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        E *const to_v = (E *)(pool_v + to_block) + (size_t)h * DP * 8;
+        if (full) {
+            E x[8][DP / 64];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const int token = (s & 3) + 4 * h + 8 * (s >> 2), slot = __builtin_amdgcn_readlane(of, token), from_page = __builtin_amdgcn_readlane(of_page, token);
+                const E *from_v = (const E *)(pool_v + kv_block_at(a.pool, from_page, u.head, slot) * ES) + (size_t)kv_half(slot & 15) * DP * 8 + kv_slot(slot & 15);
+#pragma unroll
+                for (int i = 0; i < DP / 64; ++i) x[s][i] = from_v[(lane + 64 * i) * 8];
+            }
+#pragma unroll
+            for (int i = 0; i < DP / 64; ++i) {
+                unsigned y[2 * ES];
+#pragma unroll
+                for (int c = 0; c < 2 * ES; ++c) {
+                    y[c] = 0;
+#pragma unroll
+                    for (int s = 0; s < 4 / ES; ++s) y[c] |= (unsigned)x[4 / ES * c + s][i] << (8 * ES * s);
+                }
+                Eight z;
+                __builtin_memcpy(&z, y, sizeof(z));
+                *(Eight *)(to_v + (lane + 64 * i) * 8) = z;
+            }
+            continue;
+        }
+        E x[DP / 64][8];
         bool whole = true;
+        unsigned mine = 0;  // which of the eight are written
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            const int key = (s & 3) + 4 * h + 8 * (s >> 2), of = from[key];
-            whole = whole && of >= 0;
-            x[s] = 0;
-            if (of >= 0 && page_of[key] >= 0)
-                x[s] = ((const E *)(pool_v + kv_block_at(a.pool, page_of[key], u.head, of) * ES))[eight_at(kv_half(of & 15)) + kv_slot(of & 15)];
-        }
-        E *to = (E *)vb + eight_at(h);
-        if (whole) {
-            Eight y;
-            __builtin_memcpy(&y, x, sizeof(y));
-            *(Eight *)to = y;
-        } else
+            const int token = (s & 3) + 4 * h + 8 * (s >> 2), slot = __builtin_amdgcn_readlane(of, token), from_page = __builtin_amdgcn_readlane(of_page, token);
+            if (slot >= 0) mine |= 1u << s;
+            else whole = false;
+            const E *from_v = (const E *)(pool_v + kv_block_at(a.pool, from_page >= 0 ? from_page : 0, u.head, slot >= 0 ? slot : 0) * ES) + (size_t)kv_half(slot & 15) * DP * 8 + kv_slot(slot & 15);
 #pragma unroll
-            for (int s = 0; s < 8; ++s)
-                if (from[(s & 3) + 4 * h + 8 * (s >> 2)] >= 0) to[s] = x[s];
+            for (int i = 0; i < DP / 64; ++i) {
+                x[i][s] = 0;
+                if (from_page >= 0) x[i][s] = from_v[(lane + 64 * i) * 8];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < DP / 64; ++i) {
+            if (whole) {
+                Eight y;
+                __builtin_memcpy(&y, x[i], sizeof(y));
+                *(Eight *)(to_v + (lane + 64 * i) * 8) = y;
+            } else
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    if (mine >> s & 1) to_v[(lane + 64 * i) * 8 + s] = x[i][s];
+        }
     }
-    if (FP8 && t < 32) {
-        float *scales = (t < 16 ? a.pool.ks : a.pool.vs) + u.layer * a.layer_scales;
-        const int key = t & 15, of = from[key];
-        if (of >= 0) scales[kv_scale_at(a.pool, page, u.head, at) + key] = page_of[key] >= 0 ? scales[kv_scale_at(a.pool, page_of[key], u.head, of)] : 0.f;
-    }
+    if (of >= 0)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) *(u32x4_t *)(pool_k + to_block + (((lane >> 4) + 4 * c) * 16 + key) * 16) = k[c];
+    if (FP8 && lane < 32 && of >= 0) scales[kv_scale_at(a.pool, page, u.head, at) + key] = scale;
 }
 
 extern "C" int siso_kv_evict(siso_kv *kv, int layer, const siso_kv_batch *batch, long keep, long recent, long early, float *mass, int *born, const int *to,
@@ -295,14 +420,28 @@ extern "C" int siso_kv_evict(siso_kv *kv, int layer, const siso_kv_batch *batch,
     if (each > 1L << 21) each = 1L << 21;
     if (each < 1) each = 1;
     a.from = (int *)kv->parts;
+    long room = batch->max_length > 0 && batch->max_length < a.batch.most ? batch->max_length : a.batch.most;
+    room = room < 256 ? 512 : room > KV_CHOOSE_ROOM / 2 ? KV_CHOOSE_ROOM : 2 * room;
+    // (threads: as many as have some positions each)
+    const bool few = room <= 2 * KV_CHOOSE_FEW;
+    if (!few && room * 4 > 48 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_choose<1024>, hipFuncAttributeMaxDynamicSharedMemorySize, KV_CHOOSE_ROOM * 4));
     for (a.unit0 = 0; a.unit0 < units; a.unit0 += each) {
         a.units = units - a.unit0 < each ? units - a.unit0 : each;
         a.list = a.from + a.units * keep;
-        hipLaunchKernelGGL(k_kv_choose, dim3((unsigned)a.units), dim3(KV_CHOOSE), 0, kv->stream, a);
+        if (few) hipLaunchKernelGGL(k_kv_choose<256>, dim3((unsigned)a.units), dim3(256), (size_t)room * 4, kv->stream, a, (int)room);
+        else hipLaunchKernelGGL(k_kv_choose<1024>, dim3((unsigned)a.units), dim3(1024), (size_t)room * 4, kv->stream, a, (int)room);
         KV_TRY(kv, hipGetLastError());
-        const dim3 grid((unsigned)(a.units * blocks));
-        if (kv->dtype == SISO_FP8) hipLaunchKernelGGL(k_kv_move<true>, grid, dim3(256), 0, kv->stream, a, (int)blocks);
-        else hipLaunchKernelGGL(k_kv_move<false>, grid, dim3(256), 0, kv->stream, a, (int)blocks);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.units * ((blocks + 3) / 4))), dim3(256), 0, kv->stream, a, (int)blocks); };
+        switch (kv->dp / 64 + (kv->dtype == SISO_FP8 ? 4 : 0)) {
+            case 1: go(k_kv_move<64, false>); break;
+            case 2: go(k_kv_move<128, false>); break;
+            case 3: go(k_kv_move<192, false>); break;
+            case 4: go(k_kv_move<256, false>); break;
+            case 5: go(k_kv_move<64, true>); break;
+            case 6: go(k_kv_move<128, true>); break;
+            case 7: go(k_kv_move<192, true>); break;
+            default: go(k_kv_move<256, true>); break;
+        }
         KV_TRY(kv, hipGetLastError());
     }
     return SISO_OK;
