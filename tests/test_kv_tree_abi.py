@@ -135,3 +135,22 @@ def test_tensors_that_do_not_fit(siso):  # noqa: F811
         kv.evict(b, w, 10, to=i32(2, 3))
     with pytest.raises(siso.SisoError):  # (all of it fits: there is no handle)
         kv.evict(b, w, 10, to=i32(1, 3))
+
+
+def test_stored_answers_as_a_tree(siso):  # noqa: F811
+    """near_hit's trees: what answers have in common is shared, token by token, at most so many rows."""
+    from paper_2508_18736_amd import near_hit
+
+    assert near_hit._branches([[1, 2, 3, 4], [1, 2, 5, 6], [7, 2]], 0, 6, 4) == ([1, 7, 2, 2, 3, 5], [0, 0, 1, 2, 3, 3], [1, 1, 2, 2, 3, 3])
+    assert near_hit._branches([[1, 2, 3], [9, 2, 4, 5]], 1, 9, 2) == ([2, 3, 4], [0, 1, 1], [1, 2, 2])
+    assert near_hit._branches([[1], []], 1, 4, 2) == ([], [], [])
+    assert near_hit._branches([[1, 2]], 0, 0, 2) == ([], [], [])
+
+
+@pytest.mark.parametrize("wrong", [dict(keep=-1), dict(keep=4, recent=5), dict(keep=4, recent=3, early=2), dict(keep=4, recent=-1), dict(keep=4, early=-1), dict(most=256)])
+def test_bounds_that_near_hit_refuses(siso, wrong):  # noqa: F811
+    from paper_2508_18736_amd import near_hit
+
+    target = near_hit.Target(layers=1, heads=2, vocab=50, device="cpu")
+    with pytest.raises(ValueError):
+        near_hit.serve(target, [[1, 2]], [[[3, 4], [5]]], 3, **wrong)
