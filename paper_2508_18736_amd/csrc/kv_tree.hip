@@ -313,8 +313,10 @@ __global__ __launch_bounds__(256) void k_kv_settle_all(KvSettle a) {
 }
 
 // ---------------------------------------------------------------------------- the path that stands
-// One workgroup for a sequence, a layer and a kv head.  Rows move to lower places, and in order: eight at a time are read before they are written, and
-// what is read later lies behind all that has been written.
+// One workgroup of dp threads for a sequence, a layer and a kv head.  Its first wave brings 64 rows of the path to LDS, with the pages where they are and where
+// they go.  Rows move to lower places, and in order: eight at a time are read before they are written, and what is read later lies behind all that has been
+// written.  Bound by latency: loads of the rows' numbers, the path, the page and the row wait for each other (48 paths of 5 to 30 rows, 8 layers of 8 heads in
+// 8 bits: 15.3 us; with pages read row by row and 256 threads 21).
 #define KV_KEEP_ROWS 8
 template <bool FP8>
 __global__ __launch_bounds__(256) void k_kv_keep(KvPool pool, KvBatch batch, const int *path, long layer_bytes, long layer_scales, int layers, int b0) {
@@ -326,78 +328,76 @@ __global__ __launch_bounds__(256) void k_kv_keep(KvPool pool, KvBatch batch, con
     float *const scales = FP8 ? (t & 8 ? pool.vs : pool.ks) + layer * layer_scales : nullptr;
     const int dp = pool.dp, chunks = dp * ES / 16;  // 16-byte chunks of a key
     const int *const table = batch.pages + (long)s.b * batch.width;
-    __shared__ int count, moves;  // rows of the path, and from which one on they move
-    if (t < 64) {
-        int n = 0, first = 0x7FFFFFFF, before = -1;
-        for (int j0 = 0; j0 < s.rows; j0 += 64) {
-            const int j = j0 + t, p = j < s.rows ? path[s.first + j] : -1;
-            const int up = __shfl_up(p, 1), prior = t ? up : before;
-            before = __shfl(p, 63);
-            const u64 ends = ~__ballot(p >= j && p > prior && p < s.rows);
-            const u64 moved = __ballot(p > j);
-            const int good = ends ? __ffsll((long long)ends) - 1 : 64;
-            if (moved && first == 0x7FFFFFFF) first = j0 + __ffsll((long long)moved) - 1;
-            n = j0 + good;
-            if (good < 64) break;
-        }
-        if (t == 0) {
-            count = n;
-            moves = first;
-        }
-    }
-    __syncthreads();
-    auto place = [&](int row, int &at) {  // of a row of the sequence the page, or -1
-        at = s.start + row;
-        if (at < 0 || at >= batch.most) return -1;
-        const int page = table[at >> pool.shift];
+    __shared__ int from[64], from_page[64], to_page[64];  // positions; pages or -1
+    __shared__ int count, moves;                          // rows of the path of these 64, and from which one on they move
+    auto page_of = [&](int at) {
+        const int page = at >= 0 && at < batch.most ? table[at >> pool.shift] : -1;
         if (kv_is_page(pool, page)) return page;
-        if (t == 0 && head == 0) atomicAdd(pool.bad, 1ull);
+        if (head == 0 && at >= 0 && at < batch.most) atomicAdd(pool.bad, 1ull);
         return -1;
     };
-    for (int j0 = moves; j0 < count; j0 += KV_KEEP_ROWS) {
-        const int here = count - j0 < KV_KEEP_ROWS ? count - j0 : KV_KEEP_ROWS;
-        u32x4_t k = u32x4_t{0, 0, 0, 0};
-        E v[KV_KEEP_ROWS];
-        float scale = 0.f;
-        char *k_to = nullptr;
-        int to[KV_KEEP_ROWS], to_page[KV_KEEP_ROWS];
-        float *scale_to = nullptr;
-        // values: a thread for an element of all rows
-#pragma unroll
-        for (int r = 0; r < KV_KEEP_ROWS; ++r) {
-            to_page[r] = -1;
-            to[r] = 0;
-            v[r] = 0;
-            if (r >= here) continue;
-            int at;
-            const int page = place(path[s.first + j0 + r], at);
-            to_page[r] = place(j0 + r, to[r]);
-            const int key = at & 15;
-            if (page >= 0 && t < dp) {
-                const char *block = pool_v + kv_block_at(pool, page, head, at) * ES;
-                v[r] = FP8 ? ((const E *)block)[kv_v8_at(dp, kv_half(key), t) + kv_slot(key)] : ((const E *)block)[(kv_half(key) * dp + t) * 8 + kv_slot(key)];
+    int before = -1;  // the path's last row
+    for (int base = 0; base < s.rows; base += 64) {
+        if (t < 64) {
+            const int j = base + t, p = j < s.rows ? path[s.first + j] : -1, up = __shfl_up(p, 1), prior = t ? up : before;
+            const u64 ends = ~__ballot(p >= j && p > prior && p < s.rows), moved = __ballot(p > j);
+            const int good = ends ? __ffsll((long long)ends) - 1 : 64, first = moved ? __ffsll((long long)moved) - 1 : 64;
+            before = __shfl(p, 63);
+            if (t >= first && t < good) {
+                from[t] = s.start + p;
+                from_page[t] = page_of(s.start + p);
+                to_page[t] = page_of(s.start + j);
             }
-            // keys: a thread for a chunk of a row
-            if (t / chunks == r) {
-                if (page >= 0) k = *(const u32x4_t *)(pool_k + kv_block_at(pool, page, head, at) * ES + ((t % chunks) * 16 + key) * 16);
-                if (to_page[r] >= 0) k_to = pool_k + kv_block_at(pool, to_page[r], head, to[r]) * ES + ((t % chunks) * 16 + (to[r] & 15)) * 16;
-            }
-            if (FP8 && (t & 7) == r && t < 16) {
-                if (page >= 0) scale = scales[kv_scale_at(pool, page, head, at)];
-                if (to_page[r] >= 0) scale_to = scales + kv_scale_at(pool, to_page[r], head, to[r]);
+            if (t == 0) {
+                count = good;
+                moves = first;
             }
         }
         __syncthreads();
-        if (k_to) *(u32x4_t *)k_to = k;
-        if (FP8 && scale_to) *scale_to = scale;
+        const int all = count;
+        for (int j0 = moves; j0 < all; j0 += KV_KEEP_ROWS) {
+            u32x4_t k = u32x4_t{0, 0, 0, 0};
+            E v[KV_KEEP_ROWS];
+            float scale = 0.f;
+            char *k_to = nullptr;
+            int page_to[KV_KEEP_ROWS];
+            float *scale_to = nullptr;
+            // values: a thread for an element of all rows
 #pragma unroll
-        for (int r = 0; r < KV_KEEP_ROWS; ++r) {
-            if (to_page[r] < 0 || t >= dp) continue;
-            char *block = pool_v + kv_block_at(pool, to_page[r], head, to[r]) * ES;
-            const int key = to[r] & 15;
-            ((E *)block)[FP8 ? kv_v8_at(dp, kv_half(key), t) + kv_slot(key) : (kv_half(key) * dp + t) * 8 + kv_slot(key)] = v[r];
+            for (int r = 0; r < KV_KEEP_ROWS; ++r) {
+                page_to[r] = -1;
+                v[r] = 0;
+                if (j0 + r >= all) continue;
+                const int at = from[j0 + r], to = s.start + base + j0 + r, page = from_page[j0 + r], key = at & 15;
+                page_to[r] = to_page[j0 + r];
+                if (page >= 0) {
+                    const E *block = (const E *)(pool_v + kv_block_at(pool, page, head, at) * ES);
+                    v[r] = block[FP8 ? kv_v8_at(dp, kv_half(key), t) + kv_slot(key) : (kv_half(key) * dp + t) * 8 + kv_slot(key)];
+                }
+                // keys: a thread for a chunk of a row
+                if (t / chunks == r) {
+                    if (page >= 0) k = *(const u32x4_t *)(pool_k + kv_block_at(pool, page, head, at) * ES + ((t % chunks) * 16 + key) * 16);
+                    if (page_to[r] >= 0) k_to = pool_k + kv_block_at(pool, page_to[r], head, to) * ES + ((t % chunks) * 16 + (to & 15)) * 16;
+                }
+                if (FP8 && (t & 7) == r && t < 16) {
+                    if (page >= 0) scale = scales[kv_scale_at(pool, page, head, at)];
+                    if (page_to[r] >= 0) scale_to = scales + kv_scale_at(pool, page_to[r], head, to);
+                }
+            }
+            __syncthreads();
+            if (k_to) *(u32x4_t *)k_to = k;
+            if (FP8 && scale_to) *scale_to = scale;
+#pragma unroll
+            for (int r = 0; r < KV_KEEP_ROWS; ++r) {
+                if (page_to[r] < 0) continue;
+                const int to = s.start + base + j0 + r, key = to & 15;
+                E *block = (E *)(pool_v + kv_block_at(pool, page_to[r], head, to) * ES);
+                block[FP8 ? kv_v8_at(dp, kv_half(key), t) + kv_slot(key) : (kv_half(key) * dp + t) * 8 + kv_slot(key)] = v[r];
+            }
+            // (no wait: what the next turn reads nobody has written)
         }
-        // (no wait: what the next turn reads nobody has written)
+        if (all < 64) return;
+        __syncthreads();  // (the 64 rows' places are used again)
     }
 }
 
@@ -480,7 +480,7 @@ extern "C" int siso_kv_keep(siso_kv *kv, int layer, const siso_kv_batch *batch, 
     for (long b0 = 0; b0 < b.n; b0 += each) {
         const dim3 grid((unsigned)((b.n - b0 < each ? b.n - b0 : each) * layers * kv->kv_heads));
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, kv->stream, pool, b, path, (long)kv->layer_bytes, (long)kv->layer_scales, (int)layers, (int)b0);
+            hipLaunchKernelGGL(kernel, grid, dim3(kv->dp), 0, kv->stream, pool, b, path, (long)kv->layer_bytes, (long)kv->layer_scales, (int)layers, (int)b0);
         };
         kv->dtype == SISO_FP8 ? go(k_kv_keep<true>) : go(k_kv_keep<false>);
         KV_TRY(kv, hipGetLastError());
