@@ -51,7 +51,10 @@ __device__ __forceinline__ unsigned kv_order(float mass) {
 
 // ---------------------------------------------------------------------------- which positions stay
 #define KV_CHOOSE_ROOM 32768  // words of LDS: two for each position (its number and its age), or one; of more positions both are read from memory whenever they are asked for
-#define KV_CHOOSE_FEW 2048    // positions, up to which a workgroup has 256 threads, beyond 1,024
+// Threads of a workgroup: 1,024, or 256 where there are more units than CUs, of at most so many positions each: workgroups of 1,024 that share a CU wait for
+// one another at barriers, of few positions longer than the rest takes.  Calls of 48 sequences, 8 heads (us, 256 against 1,024 threads): of 400 positions
+// 58.7 and 65.9, of 1,000 127 and 138, of 1,900 245 and 253; of 16 sequences of 1,900 93.1 and 89.9.
+#define KV_CHOOSE_FEW 2048
 // One workgroup a unit.  Its positions' numbers are brought to LDS once; the `keep`-th largest is found digit by digit (11, 11 and 10 bits), from counts of
 // each digit's values.  Each wave then goes over a stretch of the slots, in order: ranks are counts of ballots, so that nothing depends on scheduling.
 // Bound by latency: about ten passes over LDS with a barrier each behind two dependent loads (page, then mass and born).
@@ -422,8 +425,7 @@ extern "C" int siso_kv_evict(siso_kv *kv, int layer, const siso_kv_batch *batch,
     a.from = (int *)kv->parts;
     long room = batch->max_length > 0 && batch->max_length < a.batch.most ? batch->max_length : a.batch.most;
     room = room < 256 ? 512 : room > KV_CHOOSE_ROOM / 2 ? KV_CHOOSE_ROOM : 2 * room;
-    // (threads: as many as have some positions each)
-    const bool few = room <= 2 * KV_CHOOSE_FEW;
+    const bool few = room <= 2 * KV_CHOOSE_FEW && units > 256;
     if (!few && room * 4 > 48 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_choose<1024>, hipFuncAttributeMaxDynamicSharedMemorySize, KV_CHOOSE_ROOM * 4));
     for (a.unit0 = 0; a.unit0 < units; a.unit0 += each) {
         a.units = units - a.unit0 < each ? units - a.unit0 : each;
