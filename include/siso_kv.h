@@ -216,7 +216,8 @@ int siso_kv_verify_tree(siso_kv *kv, const siso_kv_batch *batch, const int *pare
  * to the place of row j, in layer `layer`, or with -1 in all of them by one call.
  *   path: device pointer, [rows] ints, as siso_kv_verify_tree leaves out_rows: increasing, with
  *         path[j] >= j (what does not keep to that ends it).
- * A sequence's pages from the one of its first row on are its own.  Asynchronous.
+ * A sequence's pages from the one of its first row on are its own.  Layers times kv_heads of one call: at most 2^23
+ * (SISO_EINVAL otherwise).  Asynchronous.
  */
 int siso_kv_keep(siso_kv *kv, int layer, const siso_kv_batch *batch, const int *path);
 
@@ -231,12 +232,13 @@ int siso_kv_keep(siso_kv *kv, int layer, const siso_kv_batch *batch, const int *
  *           noted is forgotten, for instance where a prompt's last tokens weigh all of it.)
  *   newest: device pointer, [n] ints, or NULL: length - 1 of each.  Where positions have been evicted, the true
  *           position of the newest token.
- *   decay:  0 to 1.  1: sums over all rows so far; 0: of this batch's rows alone.
+ *   decay:  0 to 1.  1: sums over all rows so far; 0: of this batch's rows alone, whatever mass held.
  *   mass:   device pointer, [layers][pages][kv_heads][page_tokens] floats: a position's is that of its slot.
  *   born:   the same of ints, or NULL.
  * A sequence without rows is left as it is, and so is all beyond its length.  No two sequences of a
- * batch may share a page.  Scores and sums are formed in single precision, the sums in an order that does not
- * depend on scheduling.  Asynchronous.
+ * batch may share a page.  Scores, within single precision's range as for siso_kv_attend, and sums are formed in single
+ * precision, the sums in an order that does not depend on scheduling.  What a row does not see does not get anything of it: infinities and
+ * NaN of a key or a row are found at the positions that the row sees.  Asynchronous.
  */
 int siso_kv_weigh(siso_kv *kv, int layer, const siso_kv_batch *batch, const void *q, long q_token_stride, long q_head_stride, int heads,
                   float scale, int window, const float *lse, const int *fresh, const int *newest, float decay, float *mass, int *born);

@@ -253,8 +253,8 @@ __device__ __forceinline__ void kv_less(const float *less, float (&l)[16]) {
         l[4 * g] = x.x, l[4 * g + 1] = x.y, l[4 * g + 2] = x.z, l[4 * g + 3] = x.w;
     }
 }
-// The powers of 8 * `groups` rows of a tile, summed for this lane's position, which they all see (a row that adds nothing has a power of zero:
-// as long as the position's keys are numbers, or another row makes the sum what they are).
+// The powers of 8 * `groups` rows of a tile, summed for this lane's position, which they all see.  What fills a tile up repeats the last row, with a
+// power of zero: nothing but what that row's own score may be comes of it.
 __device__ __forceinline__ float kv_powers(const f32x16_t &s, float scale, const float (&l)[16], int groups = 4) {
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -280,7 +280,7 @@ __device__ __forceinline__ float kv_powers_seen(const f32x16_t &s, float scale, 
 
 __device__ __forceinline__ void kv_weigh_note(const KvWeigh &a, const KvSequence &s, int pos, size_t spot, float had, float sum) {
     const int fresh = a.fresh ? a.fresh[s.b] : s.start;
-    a.mass[spot] = (pos < fresh ? a.decay * had : 0.f) + sum;
+    a.mass[spot] = (pos < fresh && a.decay > 0.f ? a.decay * had : 0.f) + sum;  // (decay 0: whatever was there)
     if (a.born && pos >= fresh) a.born[spot] = (a.newest ? a.newest[s.b] : s.length - 1) - (s.length - 1 - pos);
 }
 
@@ -335,9 +335,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 4 : 2) void k_kv_weigh_few(KvWeigh
     }
     const unsigned magic = kv_group_magic(a.group);
     for (int i = t; i < 32 * tiles * (DP / 8); i += 256) {
-        const int row = i / (DP / 8), c = i % (DP / 8), token = (int)((unsigned)row * magic >> 16);
+        const int row = i / (DP / 8), c = i % (DP / 8), of = row < work ? row : work - 1, token = (int)((unsigned)of * magic >> 16);
         u32x4_t x = u32x4_t{0, 0, 0, 0};
-        if (row < work && 8 * c < a.pool.dim) x = kv_eight_of(kv_row_at(a, k, token, row - token * a.group) + 8 * c, a.vec);
+        if (8 * c < a.pool.dim) x = kv_eight_of(kv_row_at(a, k, token, of - token * a.group) + 8 * c, a.vec);
         *(u32x4_t *)(rows + (row >> 5) * kv_tile_bytes<DP>() + (kv_piece<FP8>(c) * KV_ROWS_APART + (row & 31)) * 16) = x;
     }
     bool none = false;
@@ -509,9 +509,9 @@ __global__ __launch_bounds__(256, 2) void k_kv_weigh_rows(KvWeigh a) {
             } else {
 #pragma unroll 1
                 for (int x = t; x < ROWS * PIECES; x += 256) {
-                    const int row = x / PIECES, c = kv_unswizzled<DP>(row, x % PIECES), over = in_first + row, d = (int)((unsigned)over * magic >> 16);
+                    const int row = x / PIECES, c = kv_unswizzled<DP>(row, x % PIECES), over = in_first + (row0 + row < end ? row : end - 1 - row0), d = (int)((unsigned)over * magic >> 16);
                     u32x4_t y = u32x4_t{0, 0, 0, 0};
-                    if (row0 + row < end && 8 * c < a.pool.dim) y = kv_eight_of(q_first + (long)d * a.q_token + (long)(over - d * a.group) * a.q_head + 8 * c, 0);
+                    if (8 * c < a.pool.dim) y = kv_eight_of(q_first + (long)d * a.q_token + (long)(over - d * a.group) * a.q_head + 8 * c, 0);
                     *(u32x4_t *)(rows + buffer * STAGE + x * 16) = y;
                 }
             }
