@@ -36,255 +36,292 @@ __device__ __forceinline__ KvUnit kv_unit(const KvEvict &a, long unit) {
     u.stay = u.s.length < a.keep ? u.s.length : a.keep;
     return u;
 }
-// Where a slot's numbers are, of mass and born (of the layer); -1: its page is none.
-__device__ __forceinline__ long kv_spot(const KvPool &pool, const int *table, int head, int at) {
+// Where a slot's numbers are, of mass and born (of the layer): below 2^32, a place has 64 bytes of keys and 64 of values at least.
+#define KV_NOWHERE 0xFFFFFFFFu  // its page is none
+__device__ __forceinline__ unsigned kv_spot(const KvPool &pool, const int *table, int head, int at) {
     const int page = table[at >> pool.shift];
-    return kv_is_page(pool, page) ? (long)kv_scale_at(pool, page, head, at) : -1;
+    return kv_is_page(pool, page) ? (((unsigned)page * (unsigned)pool.kv_heads + (unsigned)head) << pool.shift) + (unsigned)(at & ((1 << pool.shift) - 1)) : KV_NOWHERE;
 }
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef int i32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
 // Numbers that are ordered as the masses are; NaN is less than all else (and 0, of positions without a page, is less than that).
 __device__ __forceinline__ unsigned kv_order(float mass) {
     const unsigned x = __float_as_uint(mass + 0.f);  // (the two zeros are equal)
     return mass != mass ? 1u : x >> 31 ? ~x : x | 0x80000000u;
 }
 
-#define KV_DIGIT 2048
-
 // ---------------------------------------------------------------------------- which positions stay
 #define KV_CHOOSE_ROOM 32768  // words of LDS: two for each position (its number and its age), or one; of more positions both are read from memory whenever they are asked for
 // Threads of a workgroup: 1,024, or 256 where there are more units than CUs, of at most so many positions each: workgroups of 1,024 that share a CU wait for
-// one another at barriers, of few positions longer than the rest takes.  Calls of 48 sequences, 8 heads (us, 256 against 1,024 threads): of 400 positions
-// 58.7 and 65.9, of 1,000 127 and 138, of 1,900 245 and 253; of 16 sequences of 1,900 93.1 and 89.9.
+// one another at barriers (8 heads, us a call with 256 and with 1,024 threads: 48 sequences of 400 positions 57 and 61, of 1,900 239 and 241, 96 of 1,000 262
+// and 271; 16 of 1,900 87 and 84).
 #define KV_CHOOSE_FEW 2048
-// One workgroup a unit.  Its positions' numbers are brought to LDS once; the `keep`-th largest is found digit by digit (11, 11 and 10 bits), from counts of
-// each digit's values.  Each wave then goes over a stretch of the slots, in order: ranks are counts of ballots, so that nothing depends on scheduling.
-// Bound by latency: about ten passes over LDS with a barrier each behind two dependent loads (page, then mass and born).
+#define KV_DIGIT 2048
+
+// Of numbers of a wave's lanes the sum of those before this lane's, and of all, in each lane.
+template <int OFF = 1>
+__device__ __forceinline__ unsigned kv_before(unsigned &all) {
+    const LanePair<unsigned> pair = lane_pair<OFF>(all);
+    const unsigned both = pair.a + pair.b, less = threadIdx.x & OFF ? both - all : 0u;
+    all = both;
+    if constexpr (OFF < 32) return less + kv_before<2 * OFF>(all);
+    else return less;
+}
+// One workgroup a unit.  Its positions' numbers are brought to LDS once, four positions a load; the `keep`-th largest is found digit by digit (11, 11 and 10 bits),
+// from counts of each digit's values, until what is left is one group.  A thread then has a stretch of the slots, in order: ranks are sums over threads, so that
+// nothing depends on scheduling.  Bound by latency: some ten passes over LDS, a barrier each, behind three loads that wait for each other (length, page, mass): 5
+// sequences of 25,683 positions down to 2,048 each, 8 heads: 18.9 us, 264 units of 900 to 1,064 13.9 us (ranks from ballots, 64 slots after 64, 29 and 17.9).
 template <int NT>
 __global__ __launch_bounds__(NT) void k_kv_choose(KvEvict a, int room) {
-    extern __shared__ unsigned numbers[];
-    __shared__ unsigned counts[KV_DIGIT];
-    constexpr int NW = NT / 64, EACH = KV_DIGIT / NT;
-    __shared__ unsigned waves[3][NW];
+    extern __shared__ __attribute__((aligned(16))) unsigned numbers[];
+    constexpr int NW = NT / 64, EACH = KV_DIGIT / NT, TURNS = 3, NEVER = -0x7FFFFFFF - 1;
+    __shared__ unsigned counts[TURNS][KV_DIGIT];
+    __shared__ unsigned waves[TURNS + 2][NW];
     __shared__ int newest_of[NW];
-    __shared__ unsigned digit, above, same_digit;
+    __shared__ int last_equal, moving;
     const KvUnit u = kv_unit(a, a.unit0 + blockIdx.x);
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), length = u.s.length, keep = a.keep;
-    int *const from = a.from + (long)blockIdx.x * keep, *const list = a.list + (long)blockIdx.x * keep;
+    int *const from = a.from + (long)blockIdx.x * keep;
     float *const mass = a.mass + u.layer * a.layer_scales;
     int *const born = a.born ? a.born + u.layer * a.layer_scales : nullptr;
     const int *const table = a.batch.pages + (long)u.s.b * a.batch.width, *const to = a.to ? a.to + (long)u.s.b * a.to_width : nullptr;
-    const int to_most = a.to_width > (SISO_KV_MOST >> a.pool.shift) ? (int)SISO_KV_MOST : (int)(a.to_width << a.pool.shift);
-    const bool all = length <= keep, cached = length <= room;
+    const int quads = (length + 3) >> 2;  // (a page has whole ones)
+    const bool all = length <= keep, cached = 4L * quads <= room, roomy = 8L * quads <= room;
     if (all && !to) return;
-    // Numbers: MANY positions of a thread at a time.
-    constexpr int MANY = 8;
-    auto each = [&](auto f) __attribute__((always_inline)) {
-        for (int i0 = t; i0 < length; i0 += MANY * NT) {
-            long at[MANY];
+    unsigned *const ages = numbers + 4 * quads;  // (if there is room)
+    for (int i = t; i < TURNS * KV_DIGIT; i += NT) counts[0][i] = 0;
+    auto largest = [](int x, int y) __attribute__((always_inline)) { return x > y ? x : y; };
+    // Four positions' places and what is there, AHEAD times; f(quad, place, weights, ages).
+    constexpr int AHEAD = 4;
+    auto each = [&](bool weights, bool times, auto f) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int q0 = t; q0 < quads; q0 += AHEAD * NT) {
+            unsigned at[AHEAD];
+            f32x4u_t weight[AHEAD];
+            i32x4u_t when[AHEAD];
 #pragma unroll
-            for (int k = 0; k < MANY; ++k) {
-                const int i = i0 + k * NT;
-                at[k] = kv_spot(a.pool, table, u.head, i < length ? i : i0);
+            for (int k = 0; k < AHEAD; ++k) at[k] = kv_spot(a.pool, table, u.head, 4 * (q0 + k * NT < quads ? q0 + k * NT : q0));
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const unsigned there = at[k] == KV_NOWHERE ? 0u : at[k];
+                if (weights) weight[k] = *(const f32x4u_t *)(mass + there);
+                if (times) when[k] = *(const i32x4u_t *)(born + there);
             }
-            f(i0, at);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (q0 + k * NT < quads) f(q0 + k * NT, at[k], weight[k], when[k]);
         }
     };
-    const bool both = born && 2L * length <= room;  // ages, too, are in LDS
-    constexpr int NEVER = -0x7FFFFFFF - 1;
     int newest = length - 1;
     if (!all && born) {
         newest = NEVER;
-        each([&](int i0, const long (&at)[MANY]) __attribute__((always_inline)) {
-            int when[MANY];
-            float weight[MANY];
+        auto note = [&](int q, unsigned at, f32x4u_t weight, i32x4u_t when) __attribute__((always_inline)) {
+            u32x4_t x, y;
 #pragma unroll
-            for (int k = 0; k < MANY; ++k) {
-                when[k] = at[k] >= 0 ? born[at[k]] : NEVER;
-                weight[k] = both && at[k] >= 0 ? mass[at[k]] : 0.f;
+            for (int j = 0; j < 4; ++j) {
+                const bool is = at != KV_NOWHERE && 4 * q + j < length;
+                y[j] = is ? when[j] : NEVER;
+                newest = largest(newest, (int)y[j]);
+                x[j] = is ? kv_order(weight[j]) : 0u;
             }
+            if (roomy) {
+                *(u32x4_t *)(numbers + 4 * q) = x;
+                *(u32x4_t *)(ages + 4 * q) = y;
+            }
+        };
+        if (roomy) each(true, true, note);
+        else each(false, true, [&](int q, unsigned at, f32x4u_t, i32x4u_t when) __attribute__((always_inline)) {
 #pragma unroll
-            for (int k = 0; k < MANY; ++k) newest = when[k] > newest ? when[k] : newest;
-            if (both)
-#pragma unroll
-                for (int k = 0; k < MANY; ++k)
-                    if (i0 + k * NT < length) {
-                        numbers[i0 + k * NT] = at[k] >= 0 ? kv_order(weight[k]) : 0u;
-                        numbers[length + i0 + k * NT] = (unsigned)when[k];
-                    }
+            for (int j = 0; j < 4; ++j) newest = largest(newest, at != KV_NOWHERE && 4 * q + j < length ? when[j] : NEVER);
         });
-        newest = wave_fold(newest, [](int x, int y) __attribute__((always_inline)) { return x > y ? x : y; });
+        newest = wave_fold(newest, largest);
         if (lane == 0) newest_of[w] = newest;
         __syncthreads();
-        newest = wave_fold(newest_of[lane & (NW - 1)], [](int x, int y) __attribute__((always_inline)) { return x > y ? x : y; });
+        newest = wave_fold(newest_of[lane & (NW - 1)], largest);
     }
     const long recent_from = (long)newest - a.recent;  // above that
     auto safe = [&](int when) { return when > recent_from || when < a.early; };
-    auto number_of = [&](long at, int when, float weight) { return at < 0 ? 0u : safe(when) ? 0xFFFFFFFFu : kv_order(weight); };
-    if (!all && both) {  // (a thread's own)
-#pragma unroll 4
-        for (int i = t; i < length; i += NT)
-            if (numbers[i] != 0 && safe((int)numbers[length + i])) numbers[i] = 0xFFFFFFFFu;
-    } else if (!all && cached)
-        each([&](int i0, const long (&at)[MANY]) __attribute__((always_inline)) {
-            int when[MANY];
-            float weight[MANY];
+    if (!all && cached) {
+        if (born && roomy) {  // (a thread's own)
+#pragma unroll 1
+            for (int q = t; q < quads; q += NT) {
+                u32x4_t x = *(const u32x4_t *)(numbers + 4 * q), y = *(const u32x4_t *)(ages + 4 * q);
 #pragma unroll
-            for (int k = 0; k < MANY; ++k) {
-                weight[k] = at[k] >= 0 ? mass[at[k]] : 0.f;
-                when[k] = !born ? i0 + k * NT : at[k] >= 0 ? born[at[k]] : 0;
+                for (int j = 0; j < 4; ++j) x[j] = x[j] != 0 && safe((int)y[j]) ? 0xFFFFFFFFu : x[j];
+                *(u32x4_t *)(numbers + 4 * q) = x;
             }
+        } else {
+            auto put = [&](int q, unsigned at, f32x4u_t weight, i32x4u_t when) __attribute__((always_inline)) {
+                u32x4_t x;
 #pragma unroll
-            for (int k = 0; k < MANY; ++k)
-                if (i0 + k * NT < length) numbers[i0 + k * NT] = number_of(at[k], when[k], weight[k]);
-        });
-    auto number = [&](int i) -> unsigned {
-        if (cached) return numbers[i];
-        const long at = kv_spot(a.pool, table, u.head, i);
-        return number_of(at, !born ? i : at >= 0 ? born[at] : 0, at >= 0 ? mass[at] : 0.f);
-    };
-    unsigned bar = 0;  // what is above it stays, and of what is equal the first `ties`
-    int ties = 0;
-    bool every = true;  // all that is equal
-    if (!all) {
-        unsigned left = keep;  // of the numbers that have the digits found so far, so many stay
-        for (int turn = 0; turn < 3; ++turn) {
-            const int shift = turn == 0 ? 21 : turn == 1 ? 10 : 0, bits = turn == 2 ? 10 : 11;
-            for (int i = t; i < KV_DIGIT; i += NT) counts[i] = 0;
-            __syncthreads();
-            for (int i0 = t; i0 < length; i0 += 4 * NT) {
-                unsigned x[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] = i0 + k * NT < length ? number(i0 + k * NT) : 0u;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (i0 + k * NT < length && (turn == 0 || (x[k] >> (shift + bits)) == (bar >> (shift + bits))))
-                        atomicAdd(&counts[(x[k] >> shift) & ((1u << bits) - 1)], 1u);
-            }
-            __syncthreads();
-            // from the top: thread t has EACH digits from KV_DIGIT - 1 - EACH t down
-            unsigned c[EACH], mine = 0;
-#pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-                c[k] = counts[KV_DIGIT - 1 - EACH * t - k];
-                mine += c[k];
-            }
-            unsigned upto = mine;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const unsigned x = __shfl_up(upto, off);
-                if (lane >= off) upto += x;
-            }
-            if (lane == 63) waves[0][w] = upto;
-            __syncthreads();
-            for (int i = 0; i < w; ++i) upto += waves[0][i];
-            if (upto - mine < left && upto >= left) {
-                unsigned ahead = upto - mine;
-#pragma unroll
-                for (int k = 0; k < EACH; ++k) {
-                    if (ahead < left && ahead + c[k] >= left) {
-                        digit = KV_DIGIT - 1 - EACH * t - k;
-                        above = ahead;
-                        same_digit = c[k];
-                    }
-                    ahead += c[k];
-                }
-            }
-            __syncthreads();
-            bar |= digit << shift;
-            left -= above;
-            every = same_digit == left;
-            if (every) break;  // (with whatever digits follow)
+                for (int j = 0; j < 4; ++j) x[j] = at == KV_NOWHERE || 4 * q + j >= length ? 0u : safe(born ? when[j] : 4 * q + j) ? 0xFFFFFFFFu : kv_order(weight[j]);
+                *(u32x4_t *)(numbers + 4 * q) = x;
+            };
+            each(true, born != nullptr, put);
         }
-        ties = (int)left;
-    }
-    // a wave's slots, 64 at a time
-    const int stretch = ((length + NT - 1) / NT) * 64, begin = w * stretch;
-    const int end = begin + stretch < length ? begin + stretch : length;
-    const u64 below = ((u64)1 << lane) - 1;
-    auto first_bits = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : ((u64)1 << n) - 1; };
-    constexpr int AHEAD = 4;  // 64 slots, so many times
-    auto in_order = [&](auto f) __attribute__((always_inline)) {
-        for (int i0 = begin; i0 < end; i0 += 64 * AHEAD) {
-            unsigned x[AHEAD];
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) x[k] = !all && i0 + 64 * k + lane < end ? number(i0 + 64 * k + lane) : 0u;
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) f(i0 + 64 * k, x[k]);
-        }
-    };
-    unsigned equal_before = 0;
-    if (!every) {
-        unsigned equal = 0;
-        in_order([&](int base, unsigned x) __attribute__((always_inline)) { equal += __popcll(__ballot(x == bar) & first_bits(end - base)); });
-        if (lane == 0) waves[0][w] = equal;
-        __syncthreads();
-        for (int i = 0; i < w; ++i) equal_before += waves[0][i];
-    }
-    unsigned equals = equal_before, hole = 0, mover = 0;
-    auto stays = [&](int base, unsigned x) __attribute__((always_inline)) {  // of the wave's next 64 slots
-        const u64 in = first_bits(end - base);
-        if (every) return (all ? ~0ull : __ballot(x >= bar)) & in;
-        const u64 same = __ballot(x == bar) & in;
-        const bool early = (same >> lane & 1) && equals + __popcll(same & below) < (unsigned)ties;
-        equals += __popcll(same);
-        return __ballot(x > bar || early) & in;
-    };
-    in_order([&](int base, unsigned x) __attribute__((always_inline)) {
-        const u64 yes = stays(base, x), low = first_bits(keep - base);
-        hole += __popcll(low & first_bits(end - base) & ~yes);
-        mover += __popcll(yes & ~low);
-    });
-    if (lane == 0) {
-        waves[1][w] = hole;
-        waves[2][w] = mover;
     }
     __syncthreads();
-    hole = mover = 0;
-    for (int i = 0; i < w; ++i) {
-        hole += waves[1][i];
-        mover += waves[2][i];
-    }
-    equals = equal_before;
-    in_order([&](int base, unsigned x) __attribute__((always_inline)) {
-        const u64 yes = stays(base, x), low = first_bits(keep - base), empties = low & first_bits(end - base) & ~yes, movings = yes & ~low;
-        const int i = base + lane;
-        if (i < keep && i < end) from[i] = empties >> lane & 1 ? -2 - (int)(hole + __popcll(empties & below)) : to ? i : -1;
-        if (movings >> lane & 1) list[mover + __popcll(movings & below)] = i;
-        hole += __popcll(empties);
-        mover += __popcll(movings);
-    });
-    __syncthreads();  // (what the workgroup has written to memory its own threads see)
-    constexpr int MOVES = 4;
-    for (int i0 = t; i0 < u.stay; i0 += MOVES * NT) {
-        int of[MOVES];
+    // What a thread has summed over its slots, before it over all threads' (`place`: one for each call).
+    auto before_all = [&](int place, unsigned mine) __attribute__((always_inline)) {
+        unsigned sum = mine;
+        const unsigned before = kv_before(sum);
+        if (lane == 0) waves[place][w] = sum;
+        __syncthreads();
+        unsigned others = lane < NW ? waves[place][lane & (NW - 1)] : 0u;
+        const unsigned ahead = kv_before(others);
+        return before + (unsigned)__builtin_amdgcn_readlane((int)ahead, w);
+    };
+    auto rest = [&](auto here) __attribute__((always_inline)) {  // `here`: the numbers are in LDS
+        constexpr bool HERE = decltype(here)::value;
+        auto four = [&](int q) {  // (what fills up the last four is less than all else)
+            if constexpr (HERE) return *(const u32x4_t *)(numbers + 4 * q);
+            u32x4_t x = u32x4_t{0, 0, 0, 0};
+            const unsigned at = kv_spot(a.pool, table, u.head, 4 * q);
+            if (at == KV_NOWHERE) return x;
+            const f32x4u_t weight = *(const f32x4u_t *)(mass + at);
+            i32x4u_t when = {4 * q, 4 * q + 1, 4 * q + 2, 4 * q + 3};
+            if (born) when = *(const i32x4u_t *)(born + at);
 #pragma unroll
-        for (int k = 0; k < MOVES; ++k) of[k] = i0 + k * NT < u.stay ? from[i0 + k * NT] : -1;
+            for (int j = 0; j < 4; ++j) x[j] = 4 * q + j >= length ? 0u : safe(when[j]) ? 0xFFFFFFFFu : kv_order(weight[j]);
+            return x;
+        };
+        unsigned bar = 0, ties = keep;  // what is above the bar stays, and of what is equal the first `ties`
+        bool every = all;               // all that is equal
+#pragma unroll 1
+        for (int turn = 0; turn < TURNS && !every; ++turn) {
+            const int shift = turn == 0 ? 21 : turn == 1 ? 10 : 0, bits = turn == 2 ? 10 : 11;
+#pragma unroll 1
+            for (int q = t; q < quads; q += NT) {
+                const u32x4_t x = four(q);
 #pragma unroll
-        for (int k = 0; k < MOVES; ++k)
-            if (of[k] <= -2) {
-                of[k] = list[-2 - of[k]];
-                from[i0 + k * NT] = of[k];
+                for (int j = 0; j < 4; ++j)
+                    if (turn == 0 || ((x[j] ^ bar) >> (shift + bits)) == 0) atomicAdd(&counts[turn][(x[j] >> shift) & ((1u << bits) - 1)], 1u);
             }
-        long at[MOVES], spot[MOVES];
-        float weight[MOVES];
-        int when[MOVES];
+            __syncthreads();
+            // from the top: thread t has EACH digits from KV_DIGIT - 1 - EACH t down.  All waves find the wave, the lane and the digit that reach `ties`.
+            auto digits_of = [&](int thread, unsigned (&c)[EACH]) __attribute__((always_inline)) {
+                unsigned sum = 0;
 #pragma unroll
-        for (int k = 0; k < MOVES; ++k) {
-            const int i = i0 + k * NT;
-            at[k] = of[k] >= 0 ? kv_spot(a.pool, table, u.head, of[k]) : -1;
-            spot[k] = of[k] < 0 || (to && i >= to_most) ? -1 : kv_spot(a.pool, to ? to : table, u.head, i);
-        }
+                for (int k = 0; k < EACH; ++k) {
+                    c[k] = counts[turn][KV_DIGIT - 1 - EACH * thread - k];
+                    sum += c[k];
+                }
+                return sum;
+            };
+            unsigned c[EACH], sum = digits_of(t, c);
+            kv_before(sum);
+            if (lane == 0) waves[turn][w] = sum;
+            __syncthreads();
+            auto reaching = [&](unsigned mine, unsigned before) { return __ffsll((long long)__ballot(before < ties && before + mine >= ties)) - 1; };
+            unsigned mine = lane < NW ? waves[turn][lane & (NW - 1)] : 0u, before;
+            sum = mine;
+            before = kv_before(sum);
+            const int of_wave = reaching(mine, before);
+            const unsigned ahead = (unsigned)__builtin_amdgcn_readlane((int)before, of_wave);
+            sum = mine = digits_of(64 * of_wave + lane, c);
+            before = ahead + kv_before(sum);
+            const int of_lane = reaching(mine, before);
+            unsigned digit = 0, above = 0, same = 0;
 #pragma unroll
-        for (int k = 0; k < MOVES; ++k) {
-            weight[k] = at[k] >= 0 ? mass[at[k]] : 0.f;
-            when[k] = born && at[k] >= 0 ? born[at[k]] : 0;
-        }
-#pragma unroll
-        for (int k = 0; k < MOVES; ++k)
-            if (spot[k] >= 0) {
-                mass[spot[k]] = weight[k];
-                if (born) born[spot[k]] = when[k];
+            for (int k = 0; k < EACH; ++k) {
+                if (before < ties && before + c[k] >= ties) {
+                    digit = KV_DIGIT - 1 - EACH * (64 * of_wave + lane) - k;
+                    above = before;
+                    same = c[k];
+                }
+                before += c[k];
             }
-    }
+            bar |= (unsigned)__builtin_amdgcn_readlane((int)digit, of_lane) << shift;
+            ties -= (unsigned)__builtin_amdgcn_readlane((int)above, of_lane);
+            every = (unsigned)__builtin_amdgcn_readlane((int)same, of_lane) == ties;  // (with whatever digits follow)
+        }
+        // a thread's slots, in order
+        const int each_of = (quads + NT - 1) / NT, begin = t * each_of, end = begin + each_of < quads ? begin + each_of : quads;
+        int cut = 0x7FFFFFFF;  // the last one of the equal ones that stay
+        if (!every) {
+            unsigned mine = 0;
+#pragma unroll 1
+            for (int q = begin; q < end; ++q) {
+                const u32x4_t x = four(q);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mine += x[j] == bar ? 1u : 0u;
+            }
+            unsigned before = before_all(TURNS, mine);
+            if (before < ties && before + mine >= ties)
+                for (int q = begin; q < end; ++q) {
+                    const u32x4_t x = four(q);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (x[j] == bar && ++before == ties) last_equal = 4 * q + j;
+                }
+            __syncthreads();
+            cut = last_equal;
+        }
+        auto stays = [&](int i, unsigned x) { return i < length && (x > bar || (x == bar && i <= cut)); };
+        unsigned so_far = 0;
+#pragma unroll 1
+        for (int q = begin; q < end; ++q) {
+            const u32x4_t x = four(q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) so_far += stays(4 * q + j, x[j]) ? 1u : 0u;
+        }
+        so_far = before_all(TURNS + 1, so_far);
+        // `where`: of a slot below `keep` -1, or (it becomes free) the number of free ones before it.  `movers`: the slots from `keep` on that stay, the last one first.
+        auto ranked = [&](int *where, int *movers) __attribute__((always_inline)) {
+            int stayed = (int)so_far;
+#pragma unroll 1
+            for (int q = begin; q < end; ++q) {
+                const u32x4_t x = four(q);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = 4 * q + j;
+                    const bool yes = stays(i, x[j]);
+                    if (i == keep) moving = keep - stayed;
+                    if (i < u.stay) where[i] = yes ? -1 : i - stayed;
+                    else if (yes) movers[keep - 1 - stayed] = i;
+                    stayed += yes;
+                }
+            }
+            __syncthreads();  // (what the workgroup has written its own threads see)
+            const int last = all ? 0 : moving - 1, to_most = a.to_width > (SISO_KV_MOST >> a.pool.shift) ? (int)SISO_KV_MOST : (int)(a.to_width << a.pool.shift);
+            constexpr int MOVES = NT == 1024 ? 2 : 4;
+#pragma unroll 1
+            for (int i0 = t; i0 < u.stay; i0 += MOVES * NT) {
+                int of[MOVES];
+                unsigned at[MOVES], spot[MOVES];
+                float weight[MOVES];
+                int when[MOVES];
+#pragma unroll
+                for (int k = 0; k < MOVES; ++k) {
+                    const int i = i0 + k * NT, rank = i < u.stay ? where[i] : -1;
+                    of[k] = rank >= 0 ? movers[last - rank] : to && i < u.stay ? i : -1;
+                    if (i < u.stay) from[i] = of[k];
+                }
+#pragma unroll
+                for (int k = 0; k < MOVES; ++k) {
+                    const int i = i0 + k * NT;
+                    at[k] = of[k] >= 0 ? kv_spot(a.pool, table, u.head, of[k]) : KV_NOWHERE;
+                    spot[k] = of[k] < 0 || (to && i >= to_most) ? KV_NOWHERE : kv_spot(a.pool, to ? to : table, u.head, i);
+                }
+#pragma unroll
+                for (int k = 0; k < MOVES; ++k) {
+                    weight[k] = at[k] != KV_NOWHERE ? mass[at[k]] : 0.f;
+                    when[k] = born && at[k] != KV_NOWHERE ? born[at[k]] : 0;
+                }
+#pragma unroll
+                for (int k = 0; k < MOVES; ++k)
+                    if (spot[k] != KV_NOWHERE) {
+                        mass[spot[k]] = weight[k];
+                        if (born) born[spot[k]] = when[k];
+                    }
+            }
+        };
+        // (where the ages were: `keep` numbers and of those that move at most length - keep)
+        if (HERE && roomy) ranked((int *)ages, (int *)ages + u.stay);
+        else ranked(from, a.list + (long)blockIdx.x * keep);
+    };
+    if (cached) rest(std::true_type{});
+    else rest(std::false_type{});
 }
 
 // ---------------------------------------------------------------------------- what moves
@@ -424,7 +461,7 @@ extern "C" int siso_kv_evict(siso_kv *kv, int layer, const siso_kv_batch *batch,
     if (each < 1) each = 1;
     a.from = (int *)kv->parts;
     long room = batch->max_length > 0 && batch->max_length < a.batch.most ? batch->max_length : a.batch.most;
-    room = room < 256 ? 512 : room > KV_CHOOSE_ROOM / 2 ? KV_CHOOSE_ROOM : 2 * room;
+    room = room < 256 ? 512 : room > KV_CHOOSE_ROOM / 2 ? KV_CHOOSE_ROOM : 2 * ((room + 3) & ~3L);
     const bool few = room <= 2 * KV_CHOOSE_FEW && units > 256;
     if (!few && room * 4 > 48 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_choose<1024>, hipFuncAttributeMaxDynamicSharedMemorySize, KV_CHOOSE_ROOM * 4));
     for (a.unit0 = 0; a.unit0 < units; a.unit0 += each) {
