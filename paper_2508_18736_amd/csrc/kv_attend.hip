@@ -169,6 +169,13 @@ __device__ __forceinline__ void kv_finish(const KvAttend &a, const KvTile &t, in
 #define KV_STRETCHES 1024
 #define KV_LEAST 4  // units of a stretch, at least, one for each wave (one token of 2,001 positions gets 5: the launch has no workgroup for the last part of 4, and the fifth
                     // unit is a second step of one wave)
+// Trees of up to 128 elements go to the chunks' kernel where its tiles of 256 rows are filled by half, the work is not light, and there are so few tiles (those that
+// are likely) that they are cut into pieces of one length (heads of 128, 4 rows of work for each new one over 8 kv heads, us by the first kernel and by the
+// chunks': one tree of 256 rows behind 4,000 positions 45 and 47, behind 8,000 64 and 59, in 8 bits behind 30,000 182 and 156; 3 of 40 behind 9,000 to
+// 20,000 84 and 68, 3 of 24 behind 30,000 122 and 145; 8 of 100 behind 4,000 126 and 105; 12 of 60 to 100 behind 1,000 to 5,000 98 and 107, in 8 bits 87
+// and 117; 24 of 35 to 64 in 8 bits 151 and 176).
+#define KV_TREE_LIGHT (250L << 20)
+#define KV_TREE_TILES 160
 #define KV_TREE_WHOLE 20
 #define KV_TREE_ROOT 2.0f
 #define KV_ENOUGH 32 // units that are worth being joined
@@ -358,11 +365,24 @@ __global__ __launch_bounds__(256, DP <= 64 && FP8 ? 4 : DP <= 128 ? 2 : 1) void 
         count = __builtin_amdgcn_readlane(cuts, at);
         const unsigned in = item - __builtin_amdgcn_readlane(upto - mine, at);
         if (in >= (unsigned)__builtin_amdgcn_readlane(mine, at)) return;  // (more tiles than 32 bits count)
-        // heads first, then pieces: neighbours read the same pages
-        const unsigned rest = __builtin_amdgcn_readfirstlane(in / (unsigned)a.pool.kv_heads);
-        head = in - rest * a.pool.kv_heads;
-        const unsigned tile = __builtin_amdgcn_readfirstlane(rest / (unsigned)count);
-        piece = rest - tile * count;
+        unsigned tile;
+        if constexpr (TREE) {
+            // All tiles read the same stretches: those of a stretch and head follow each other at a distance of eight, so that one XCD reads it once (2 trees of
+            // 30 to 50 rows, 4 heads for each of 8, behind 30,000 positions: 115 us, tile after tile 140).
+            const unsigned tiles = (unsigned)(t.s.rows * a.group + 31) >> 5, units = (unsigned)(count * a.pool.kv_heads);
+            const unsigned eight = __builtin_amdgcn_readfirstlane(in / (8 * tiles)), rest = in - 8 * tiles * eight;
+            const unsigned wide = units - 8 * eight < 8 ? units - 8 * eight : 8;
+            tile = __builtin_amdgcn_readfirstlane(rest / wide);
+            const unsigned unit = 8 * eight + rest - tile * wide;
+            piece = __builtin_amdgcn_readfirstlane(unit / (unsigned)a.pool.kv_heads);
+            head = unit - piece * a.pool.kv_heads;
+        } else {
+            // heads first, then pieces: neighbours read the same pages
+            const unsigned rest = __builtin_amdgcn_readfirstlane(in / (unsigned)a.pool.kv_heads);
+            head = in - rest * a.pool.kv_heads;
+            tile = __builtin_amdgcn_readfirstlane(rest / (unsigned)count);
+            piece = rest - tile * count;
+        }
         first_part = __builtin_amdgcn_readlane(upto_parts - my_parts, at) + (tile * a.pool.kv_heads + head) * count;
         kv_tile<TREE>(a, tile * 32, 32, t);
         int base;
@@ -769,8 +789,14 @@ struct KvChunk {
 
 struct KvPieces {
     long slots, slot0;
-    int ways;  // a tile's positions are cut into at most so many pieces
-    int per;   // (trees) of so many blocks at least
+    int ways;      // a tile's positions are cut into at most so many pieces
+    int at_once;   // (trees) workgroups that run at once
+    int room;      // parts that the workspace holds
+};
+struct KvPiece {
+    int head, piece, pieces;
+    int from, blocks, per;  // where the tile's positions begin, its blocks of KEYS positions, those of a piece
+    long part, next_part;   // where the tile's first part is, and how far apart they are
 };
 #define KV_PIECE_LEAST 256  // positions
 // A phase of products: operands are read so many products ahead (4: 1% slower, 8: 2%), and the work of the next stages begins behind this one.
@@ -791,10 +817,92 @@ __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces 
     from = t.lo & ~15;  // (no block that nobody sees: its page may be given up)
     blocks = t.hi > from ? (t.hi - from + KEYS - 1) / KEYS : 0;
     per = (blocks + p.ways - 1) / p.ways;
-    if (TREE && per < p.per) per = p.per;
     if (per < KV_PIECE_LEAST / KEYS) per = KV_PIECE_LEAST / KEYS;
     pieces = blocks > 0 ? (blocks + per - 1) / per : 1;
     return true;
+}
+
+// Trees of up to 64 sequences: every workgroup knows all lengths, and cuts the tiles so that all pieces together are as many as run at once, or twice as many,
+// and so on where there are more tiles than that: the smallest number of blocks with which they are no more.  (`tile_of`: number `index` counts tiles
+// and heads, not pieces.)  All tiles of a sequence go by its whole length.  False: there are not as many.
+// (24 trees of 35 to 64 rows, 4 heads for each of 8, behind 2,000 to 6,000 positions in 8 bits: 176 us, cut by the tiles that are likely 227.)
+template <int ROWS, int KEYS>
+__device__ __forceinline__ bool kv_tree_piece(const KvAttend &a, const KvPieces &p, long index, bool tile_of, KvTile &t, KvPiece &k) {
+    const int lane = threadIdx.x & 63, heads = a.pool.kv_heads;
+    const KvSequence s = kv_sequence(a.batch, lane < a.batch.n ? lane : a.batch.n - 1);
+    const bool has = lane < a.batch.n && s.rows > 0 && s.rows <= SISO_KV_TREE;
+    const int from = kv_window_from(a, s.start) & ~15;  // (no block that nobody sees: its page may be given up)
+    const unsigned tiles = has ? ((unsigned)(s.rows * a.group) + ROWS - 1) / ROWS * (unsigned)heads : 0u;
+    const unsigned blocks = s.length > from ? ((unsigned)(s.length - from) + KEYS - 1) / KEYS : 1u;
+    auto sum = [](auto v) __attribute__((always_inline)) { return wave_fold(v, [](auto x, auto y) __attribute__((always_inline)) { return x + y; }); };
+    auto most = [](unsigned v) __attribute__((always_inline)) { return wave_fold(v, [](unsigned x, unsigned y) __attribute__((always_inline)) { return x > y ? x : y; }); };
+    const unsigned all = sum(tiles), top = most(tiles ? blocks : 1u), goal = (all + p.at_once - 1) / p.at_once * p.at_once;
+    unsigned per = top;
+    if (tile_of) per = *(const unsigned *)a.plan;  // (what the pieces' workgroups found)
+    else if (goal <= (unsigned)p.room) {
+        const u64 work = sum((u64)tiles * blocks);
+        unsigned low = (unsigned)((work + goal - 1) / goal);  // (fewer are too many pieces)
+        if (low < KV_PIECE_LEAST / KEYS) low = KV_PIECE_LEAST / KEYS;
+        while (low < per) {
+            const unsigned middle = (low + per) / 2;
+            if (sum(tiles * ((blocks + middle - 1) / middle)) <= goal) per = middle;
+            else low = middle + 1;
+        }
+        per = per > low ? per : low;
+    }
+    per = __builtin_amdgcn_readfirstlane(per);
+    if (!tile_of && index == 0 && threadIdx.x == 0) *(unsigned *)a.plan = per;
+    const unsigned pieces = (blocks + per - 1) / per, mine = tile_of ? tiles : tiles * pieces;
+    unsigned upto = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const unsigned x = __shfl_up(upto, off);
+        if (lane >= off) upto += x;
+    }
+    unsigned before_parts = upto - mine;  // parts of the sequences before
+    if (tile_of) {
+        before_parts = tiles * pieces;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const unsigned x = __shfl_up(before_parts, off);
+            if (lane >= off) before_parts += x;
+        }
+        before_parts -= tiles * pieces;
+    }
+    const u64 over = __ballot((long)upto > index);
+    if (over == 0) return false;
+    const int at = __ffsll((long long)over) - 1;
+    t.s.b = at;
+    t.s.first = __builtin_amdgcn_readlane(s.first, at);
+    t.s.rows = __builtin_amdgcn_readlane(s.rows, at);
+    t.s.length = __builtin_amdgcn_readlane(s.length, at);
+    t.s.start = t.s.length - t.s.rows;
+    const unsigned in = (unsigned)index - (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), at), of_tiles = (unsigned)__builtin_amdgcn_readlane((int)tiles, at);
+    k.piece = (int)(in / of_tiles);  // heads first, then tiles: neighbours read the same pages
+    const unsigned tile = in - (unsigned)k.piece * of_tiles;
+    k.head = (int)(tile % (unsigned)heads);
+    k.pieces = __builtin_amdgcn_readlane((int)pieces, at);
+    k.from = __builtin_amdgcn_readlane(from, at);
+    k.blocks = __builtin_amdgcn_readlane((int)blocks, at);
+    k.per = (int)per;
+    k.part = (long)(unsigned)__builtin_amdgcn_readlane((int)before_parts, at) + tile;
+    k.next_part = of_tiles;
+    kv_tile<true>(a, (int)(tile / (unsigned)heads) * ROWS, ROWS, t);
+    return true;
+}
+// The piece of a workgroup of k_kv_attend_chunk, or the tile of one of k_kv_attend_join (`tile_of`).
+template <int ROWS, int KEYS, bool TREE>
+__device__ __forceinline__ bool kv_chunk_piece(const KvAttend &a, const KvPieces &p, bool tile_of, KvTile &t, KvPiece &k) {
+    if constexpr (TREE)
+        if (a.batch.n <= 64) return kv_tree_piece<ROWS, KEYS>(a, p, p.slot0 + blockIdx.x, tile_of, t, k);
+    // (the tiles of one kv head follow each other at a distance of kv_heads, those that see most first)
+    const int heads = a.pool.kv_heads, ways = tile_of ? 1 : p.ways;
+    const long at_slot = blockIdx.x / (heads * ways);
+    k.head = blockIdx.x % heads;
+    k.piece = blockIdx.x / heads % ways;
+    k.part = at_slot * p.ways * heads + k.head;
+    k.next_part = heads;
+    return kv_chunk_tile<ROWS, KEYS, TREE>(a, p, p.slot0 + p.slots - 1 - at_slot, t, k.from, k.blocks, k.per, k.pieces) && k.piece < k.pieces;
 }
 
 template <int DP, bool FP8, bool TREE>
@@ -803,13 +911,10 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
     constexpr int KEYS = C::KEYS, SUBS = C::SUBS, BLOCKS = C::BLOCKS, NS = C::NS, NU = C::NU, NL = C::NL;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
-    // (the tiles of one kv head follow each other at a distance of kv_heads, those that see most first)
-    const int head = blockIdx.x % a.pool.kv_heads, piece = blockIdx.x / a.pool.kv_heads % p.ways;
-    const long slot = p.slot0 + p.slots - 1 - blockIdx.x / (a.pool.kv_heads * p.ways);
     KvTile t;
-    int from, blocks, per, pieces;
-    if (!kv_chunk_tile<C::ROWS, KEYS, TREE>(a, p, slot, t, from, blocks, per, pieces) || piece >= pieces) return;
-    const int first = from + piece * per * KEYS, stages = blocks - piece * per < per ? blocks - piece * per : per;
+    KvPiece k;
+    if (!kv_chunk_piece<C::ROWS, KEYS, TREE>(a, p, false, t, k)) return;
+    const int head = k.head, pieces = k.pieces, done = k.piece * k.per, first = k.from + done * KEYS, stages = k.blocks - done < k.per ? k.blocks - done : k.per;
 
     // this wave's rows; `any`: there are some
     const bool any = w * 32 < t.rows;
@@ -1163,13 +1268,13 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
     const int r = w * 32 + n;  // of the tile
     const float sum = kv_both_halves_sum(l), top = m * a.scale;
     if (pieces > 1) {
-        float *part = a.parts + (size_t)blockIdx.x * KV_CHUNK_PART(C::ROWS, DP);
+        float *part = a.parts + (size_t)(k.part + k.piece * k.next_part) * KV_CHUNK_PART(C::ROWS, DP);
         if (!valid) return;
 #pragma unroll
         for (int u = 0; u < NU; ++u)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *(float4 *)(part + r * DP + 32 * u + 8 * g + 4 * h) = make_float4(o[u][4 * g], o[u][4 * g + 1], o[u][4 * g + 2], o[u][4 * g + 3]);
+                if (32 * u + 8 * g < a.pool.dim) *(float4 *)(part + r * DP + 32 * u + 8 * g + 4 * h) = make_float4(o[u][4 * g], o[u][4 * g + 1], o[u][4 * g + 2], o[u][4 * g + 3]);
         if (h == 0) *(float2 *)(part + C::ROWS * DP + 2 * r) = make_float2(top, sum);
         return;
     }
@@ -1197,24 +1302,37 @@ __global__ __launch_bounds__((KvChunk<DP, FP8>::NT), (KvChunk<DP, FP8>::PER_SIMD
 template <int DP, bool FP8, bool TREE>
 __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) {
     using C = KvChunk<DP, FP8>;
-    const int head = blockIdx.x % a.pool.kv_heads;
-    const long at_slot = blockIdx.x / a.pool.kv_heads;
     KvTile t;
-    int from, blocks, per, pieces;
-    if (!kv_chunk_tile<C::ROWS, C::KEYS, TREE>(a, p, p.slot0 + p.slots - 1 - at_slot, t, from, blocks, per, pieces) || pieces <= 1) return;
-    const float *parts = a.parts + (size_t)(at_slot * p.ways * a.pool.kv_heads + head) * KV_CHUNK_PART(C::ROWS, DP);
-    const size_t next = (size_t)a.pool.kv_heads * KV_CHUNK_PART(C::ROWS, DP);
+    KvPiece k;
+    if (!kv_chunk_piece<C::ROWS, C::KEYS, TREE>(a, p, true, t, k) || k.pieces <= 1) return;
+    const int head = k.head, pieces = k.pieces;
+    const float *parts = a.parts + (size_t)k.part * KV_CHUNK_PART(C::ROWS, DP);
+    const size_t next = (size_t)k.next_part * KV_CHUNK_PART(C::ROWS, DP);
     const int i = blockIdx.y * 256 + threadIdx.x;
-    if (i < t.rows * (DP / 4)) {
-        const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+    const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+    if (r < t.rows && d < a.pool.dim) {
         float top = -INFINITY, sum = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-        for (int s = 0; s < pieces; ++s) top = fmaxf(top, parts[s * next + C::ROWS * DP + 2 * r]);
-#pragma unroll 8
-        for (int s = 0; s < pieces; ++s) {
-            const float2 ml = *(const float2 *)(parts + s * next + C::ROWS * DP + 2 * r);
-            kv_add_part(ml.x, top, ml.y, *(const float4 *)(parts + s * next + r * DP + d), sum, x);
+        constexpr int MANY = 4;  // pieces whose loads do not wait for each other
+        for (int s0 = 0; s0 < pieces; s0 += MANY) {
+            float y[MANY];
+#pragma unroll
+            for (int k = 0; k < MANY; ++k) y[k] = parts[(s0 + k < pieces ? s0 + k : s0) * next + C::ROWS * DP + 2 * r];
+#pragma unroll
+            for (int k = 0; k < MANY; ++k) top = fmaxf(top, y[k]);
+        }
+        for (int s0 = 0; s0 < pieces; s0 += MANY) {
+            float2 ml[MANY];
+            float4 y[MANY];
+#pragma unroll
+            for (int k = 0; k < MANY; ++k) {
+                const float *part = parts + (s0 + k < pieces ? s0 + k : s0) * next;
+                ml[k] = *(const float2 *)(part + C::ROWS * DP + 2 * r);
+                y[k] = *(const float4 *)(part + r * DP + d);
+            }
+#pragma unroll
+            for (int k = 0; k < MANY; ++k)
+                if (s0 + k < pieces) kv_add_part(ml[k].x, top, ml[k].y, y[k], sum, x);
         }
         kv_finish(a, t, head, r, d, top, sum, x);
     }
@@ -1224,28 +1342,34 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(KvAttend a, KvPieces p) 
 static int kv_chunk_workgroups(int dp) { return dp == 64 ? 512 : 256; }
 
 template <int DP, bool FP8, bool TREE>
-static int attend_chunks(siso_kv *kv, const KvAttend &a, long max_length, long max_new) {
+static int attend_chunks(siso_kv *kv, const KvAttend &a) {
     using C = KvChunk<DP, FP8>;
     KvPieces p;
-    p.per = 0;
     p.slots = kv_slots_before(a.batch.rows, a.batch.n, a.group, C::ROWS == 256 ? 8 : 7, 1);
     const long tiles = p.slots * kv->kv_heads, room = (long)(SISO_KV_PARTS / KV_CHUNK_PART(C::ROWS, DP));
     long ways = tiles <= kv_chunk_workgroups(DP) / 2 ? kv_chunk_workgroups(DP) / tiles : 1;
-    if constexpr (TREE) {
-        // There are about half as many tiles as there may be (one more for each sequence), or, where all have as many rows, so many; pieces are alike,
-        // whatever the lengths are.
-        const long rows = (long)a.batch.rows * a.group / C::ROWS, same = a.batch.n * ((max_new * a.group + C::ROWS - 1) / C::ROWS);
-        const long likely = (a.batch.rows >= max_new * a.batch.n ? same : rows + (a.batch.n + 1) / 2) * kv->kv_heads;
-        ways = (kv_chunk_workgroups(DP) + likely - 1) / likely;  // (twice as many: 4 trees of 256 rows behind 8,000 positions 185 us, not 164)
-        const long seen = a.window > 0 && a.window + 256L < max_length ? a.window + 256L : max_length, blocks = (seen + C::KEYS - 1) / C::KEYS;
-        p.per = (int)((blocks + ways - 1) / ways);
-    }
     if (ways > room / tiles) ways = room / tiles;
     if (ways > 64) ways = 64;
     if (ways < 1) ways = 1;
     p.ways = (int)ways;
     constexpr int LDS = C::LDS + (TREE ? C::MASKS : 0);
     if (LDS > 64 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_attend_chunk<DP, FP8, TREE>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+    p.at_once = kv_chunk_workgroups(DP);
+    p.room = (int)room;
+    if (TREE && a.batch.n <= 64) {
+        // There are at most `tiles`; how many pieces the device makes of them it knows by itself.
+        auto rounds = [&](long of) { return (of + p.at_once - 1) / p.at_once * p.at_once; };
+        auto launch = [&](auto kernel, long all, int threads, int high, int shared) {
+            const long most = (1L << 31) / threads / high;
+            for (p.slot0 = 0; p.slot0 < all; p.slot0 += most)
+                hipLaunchKernelGGL(kernel, dim3((unsigned)(all - p.slot0 < most ? all - p.slot0 : most), high), dim3(threads), shared, kv->stream, a, p);
+        };
+        launch(k_kv_attend_chunk<DP, FP8, TREE>, rounds(tiles), C::NT, 1, LDS);
+        KV_TRY(kv, hipGetLastError());
+        if (rounds((long)a.batch.rows * a.group / C::ROWS * kv->kv_heads) <= room) launch(k_kv_attend_join<DP, FP8, TREE>, tiles, 256, C::ROWS * (DP / 4) / 256, 0);
+        KV_TRY(kv, hipGetLastError());
+        return SISO_OK;
+    }
     const long slots = p.slots, piece = ((1L << 31) / C::NT) / (kv->kv_heads * ways);  // (a launch has fewer than 2^32 threads)
     for (p.slot0 = 0; p.slot0 < slots; p.slot0 += piece) {
         p.slots = slots - p.slot0 < piece ? slots - p.slot0 : piece;
@@ -1265,12 +1389,15 @@ static int attend(siso_kv *kv, KvAttend &a, long max_length, long max_new) {
     const long seen = a.window > 0 && a.window + 32L < max_length ? a.window + 32L : max_length;
     const long light = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads * seen;
     bool by_few = DP <= 128 && light * DP <= (a.batch.rows >= max_new * a.batch.n ? KV_LIGHT : KV_LIGHT_MIXED);
-    // (trees: whatever the work is, if they do not fill the chunks' tiles; 24 trees of 5 to 64 rows, 4 heads for each: 72 us, by chunks 153)
-    if (TREE) by_few = DP <= 128 && (light * DP <= KV_LIGHT || (long)a.batch.rows * a.group < 192L * a.batch.n);
-    a.few = by_few ? 1 << 30 : KV_FEW;
+    if (TREE) {  // all by one kernel (both, each for its own, took 5 to 20% longer than the chunks' alone)
+        const long tiles = ((long)a.batch.rows * a.group / KvChunk<DP, FP8>::ROWS + (a.batch.n + 1) / 2) * kv->kv_heads;
+        by_few = max_new * a.group <= KV_FEW ||
+                 (DP <= 128 && (light * DP <= KV_TREE_LIGHT || tiles > KV_TREE_TILES || (long)a.batch.rows * a.group < KV_FEW * (long)a.batch.n));
+    }
+    a.few = by_few ? 1 << 30 : TREE ? 0 : KV_FEW;
     if (max_new * a.group > a.few) {
-        const int rc = attend_chunks<DP, FP8, TREE>(kv, a, max_length, max_new);
-        if (rc != SISO_OK || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
+        const int rc = attend_chunks<DP, FP8, TREE>(kv, a);
+        if (rc != SISO_OK || TREE || a.batch.rows >= max_new * a.batch.n) return rc;  // (all have max_new rows)
     }
     constexpr int KS = kv_step<DP, FP8>();
     const long tiles = (((long)a.batch.rows * a.group >> 5) + a.batch.n) * kv->kv_heads, cuts = (max_length / KS + 2 + KV_LEAST - 1) / KV_LEAST;
