@@ -11,7 +11,7 @@ import kv_oracle
 import kv_tree_oracle as oracle
 from gpu_util import DEV
 from test_gpu_kv import Setup, ends, ints, siso  # noqa: F401
-from test_gpu_kv_tree import random_tree
+from test_kv_gpu_tree import random_tree
 
 pytestmark = pytest.mark.gpu
 

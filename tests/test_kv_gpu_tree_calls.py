@@ -10,9 +10,9 @@ import kv_oracle
 import kv_tree_oracle as oracle
 from gpu_util import DEV
 from test_gpu_kv import ends, ints, siso  # noqa: F401
-from test_gpu_kv_evict import Full
-from test_gpu_kv_tree import Trees, random_tree
-from test_gpu_kv_weigh import Weighed
+from test_kv_gpu_evict import Full
+from test_kv_gpu_tree import Trees, random_tree
+from test_kv_gpu_weigh import Weighed
 
 pytestmark = pytest.mark.gpu
 

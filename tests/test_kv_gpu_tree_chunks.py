@@ -10,7 +10,7 @@ import kv_oracle
 import kv_tree_oracle as oracle
 from gpu_util import DEV
 from test_gpu_kv import ends, ints, siso  # noqa: F401
-from test_gpu_kv_tree import Trees
+from test_kv_gpu_tree import Trees
 
 pytestmark = pytest.mark.gpu
 
