@@ -791,7 +791,7 @@ struct KvPieces {
     long slots, slot0;
     int ways;      // a tile's positions are cut into at most so many pieces
     int at_once;   // (trees) workgroups that run at once
-    int room;      // parts that the workspace holds
+    int room;      // parts that the workspace holds (0: no tile is cut)
 };
 struct KvPiece {
     int head, piece, pieces;
@@ -833,10 +833,12 @@ __device__ __forceinline__ bool kv_tree_piece(const KvAttend &a, const KvPieces 
     const bool has = lane < a.batch.n && s.rows > 0 && s.rows <= SISO_KV_TREE;
     const int from = kv_window_from(a, s.start) & ~15;  // (no block that nobody sees: its page may be given up)
     const unsigned tiles = has ? ((unsigned)(s.rows * a.group) + ROWS - 1) / ROWS * (unsigned)heads : 0u;
-    const unsigned blocks = s.length > from ? ((unsigned)(s.length - from) + KEYS - 1) / KEYS : 1u;
+    const unsigned blocks = s.length > from ? ((unsigned)(s.length - from) + KEYS - 1) / KEYS : 0u;
     auto sum = [](auto v) __attribute__((always_inline)) { return wave_fold(v, [](auto x, auto y) __attribute__((always_inline)) { return x + y; }); };
     auto most = [](unsigned v) __attribute__((always_inline)) { return wave_fold(v, [](unsigned x, unsigned y) __attribute__((always_inline)) { return x > y ? x : y; }); };
-    const unsigned all = sum(tiles), top = most(tiles ? blocks : 1u), goal = (all + p.at_once - 1) / p.at_once * p.at_once;
+    const unsigned all = sum(tiles), top = most(tiles && blocks ? blocks : 1u), goal = (all + p.at_once - 1) / p.at_once * p.at_once;
+    if (all == 0) return false;
+    auto cut = [&](unsigned by) __attribute__((always_inline)) { return blocks ? (blocks + by - 1) / by : 1u; };
     unsigned per = top;
     if (tile_of) per = *(const unsigned *)a.plan;  // (what the pieces' workgroups found)
     else if (goal <= (unsigned)p.room) {
@@ -845,14 +847,14 @@ __device__ __forceinline__ bool kv_tree_piece(const KvAttend &a, const KvPieces 
         if (low < KV_PIECE_LEAST / KEYS) low = KV_PIECE_LEAST / KEYS;
         while (low < per) {
             const unsigned middle = (low + per) / 2;
-            if (sum(tiles * ((blocks + middle - 1) / middle)) <= goal) per = middle;
+            if (sum(tiles * cut(middle)) <= goal) per = middle;
             else low = middle + 1;
         }
         per = per > low ? per : low;
     }
     per = __builtin_amdgcn_readfirstlane(per);
     if (!tile_of && index == 0 && threadIdx.x == 0) *(unsigned *)a.plan = per;
-    const unsigned pieces = (blocks + per - 1) / per, mine = tile_of ? tiles : tiles * pieces;
+    const unsigned pieces = cut(per), mine = tile_of ? tiles : tiles * pieces;
     unsigned upto = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -1364,9 +1366,11 @@ static int attend_chunks(siso_kv *kv, const KvAttend &a) {
             for (p.slot0 = 0; p.slot0 < all; p.slot0 += most)
                 hipLaunchKernelGGL(kernel, dim3((unsigned)(all - p.slot0 < most ? all - p.slot0 : most), high), dim3(threads), shared, kv->stream, a, p);
         };
+        const bool join = rounds((long)a.batch.rows * a.group / C::ROWS * kv->kv_heads) <= room;
+        if (!join) p.room = 0;  // (more tiles than that are cut)
         launch(k_kv_attend_chunk<DP, FP8, TREE>, rounds(tiles), C::NT, 1, LDS);
         KV_TRY(kv, hipGetLastError());
-        if (rounds((long)a.batch.rows * a.group / C::ROWS * kv->kv_heads) <= room) launch(k_kv_attend_join<DP, FP8, TREE>, tiles, 256, C::ROWS * (DP / 4) / 256, 0);
+        if (join) launch(k_kv_attend_join<DP, FP8, TREE>, tiles, 256, C::ROWS * (DP / 4) / 256, 0);
         KV_TRY(kv, hipGetLastError());
         return SISO_OK;
     }

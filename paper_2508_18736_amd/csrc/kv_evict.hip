@@ -463,7 +463,7 @@ extern "C" int siso_kv_evict(siso_kv *kv, int layer, const siso_kv_batch *batch,
     long room = batch->max_length > 0 && batch->max_length < a.batch.most ? batch->max_length : a.batch.most;
     room = room < 256 ? 512 : room > KV_CHOOSE_ROOM / 2 ? KV_CHOOSE_ROOM : 2 * ((room + 3) & ~3L);
     const bool few = room <= 2 * KV_CHOOSE_FEW && units > 256;
-    if (!few && room * 4 > 48 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_choose<1024>, hipFuncAttributeMaxDynamicSharedMemorySize, KV_CHOOSE_ROOM * 4));
+    if (!few && room * 4 > 32 * 1024) KV_TRY(kv, hipFuncSetAttribute((const void *)k_kv_choose<1024>, hipFuncAttributeMaxDynamicSharedMemorySize, KV_CHOOSE_ROOM * 4));
     for (a.unit0 = 0; a.unit0 < units; a.unit0 += each) {
         a.units = units - a.unit0 < each ? units - a.unit0 : each;
         a.list = a.from + a.units * keep;

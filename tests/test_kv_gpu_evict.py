@@ -231,3 +231,11 @@ def test_in_a_graph(siso):  # noqa: F811
             eager = step()
             torch.cuda.synchronize()
             assert all(torch.equal(x, y) for x, y in zip(replayed, eager)), f"replay {turn}"
+
+
+@pytest.mark.parametrize("length", [4090, 5119, 5121, 5600, 6144, 6145, 8191, 16384, 16385, 32768, 32769])
+def test_lengths_where_the_room_in_shared_memory_changes(siso, length):  # noqa: F811
+    print(f"case: evict {length}", flush=True)
+    s = Full(siso, "fp8", 8, 1, 128, [length, 3], seed=length % 100, kind="ties" if length % 2 else "spread")
+    s.all = s.kv.batch(ends(s.length), s.length_dev, s.pages, max_length=length)
+    s.check(length // 3, 100, 4, label=str(length))

@@ -145,3 +145,33 @@ def test_replayed_with_other_lengths(siso):  # noqa: F811
                 want = oracle.attend(q[at:at + m].cpu(), hk[r], hv[r], oracle.seen_by(oracle.ancestors(s.parents[b]), l), float(torch.tensor(128 ** -0.5)))
                 kv_oracle.check_attend(out[at:at + m], lse[at:at + m], want, 128, f"{lengths} sequence {b}")
                 at += m
+
+
+def test_sequences_without_positions(siso):  # noqa: F811
+    """Rows of sequences without tokens, or with fewer tokens than rows, among others: zeros and minus infinity where nothing is seen."""
+    print("case: heavy trees, no positions", flush=True)
+    s = Heavy(siso, "bf16", 128, 1, 16, [200, 100, 0, 256, 90], [0, 1500, 0, 100, 90], seed=21)
+    s.write()
+    s.check_tree(s.queries(4), label="no positions")
+    s.check_tree(s.queries(4), window=1000000, label="no positions, window")
+
+
+def test_a_sequence_of_too_many_rows_among_many_tiles(siso):  # noqa: F811
+    """It is left out; the others, whose tiles are more than are ever cut or fewer, are whole."""
+    print("case: heavy trees, too many rows", flush=True)
+    new, length = [256] * 3 + [3000], [300, 1700, 256, 3000]
+    s = Heavy(siso, "bf16", 136, 8, 16, new[:3] + [2], length, seed=22)
+    s.write()
+    q = torch.cat([s.queries(64)[:768], torch.zeros(3000, 64, 136, dtype=torch.bfloat16)])
+    batch = s.kv.batch(ends(new), s.length_dev, s.pages, max_new=256)
+    parent = torch.cat([s.tree.parent[:768], torch.zeros(3000, dtype=torch.int32, device=DEV)])
+    out, lse = s.kv.attend(batch, q.to(DEV), with_lse=True, tree=s.kv.tree(batch, parent))
+    hk, hv = kv_oracle.held(s.k, "bf16"), kv_oracle.held(s.v, "bf16")
+    for b in range(3):
+        at, r = 256 * b, slice(s.starts[b], s.starts[b] + length[b])
+        rows = [0, 1, 31, 100, 128, 200, 255]
+        lists = [x if i in rows else [] for i, x in enumerate(oracle.ancestors(s.parents[b]))]
+        seen = oracle.seen_by(lists, length[b])
+        seen[[i for i in range(256) if i not in rows]] = False
+        want = oracle.attend(q[at:at + 256], hk[r], hv[r], seen, float(torch.tensor(136 ** -0.5)))
+        kv_oracle.check_attend(out[at:at + 256][rows], lse[at:at + 256][rows], [x[rows] for x in want], 136, f"sequence {b}")
