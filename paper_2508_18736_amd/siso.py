@@ -700,7 +700,7 @@ class PagedKV:
         rows = batch.rows
         self._vec(parent, torch.int32, (rows,), "parent")
         mask = torch.empty((rows, TREE // 32), dtype=torch.int32, device=self.device)
-        depth = torch.empty(rows, dtype=torch.int32, device=self.device)
+        depth = torch.empty_like(parent)
         if self._elsewhere():
             self._used(parent, mask, depth, batch.first)
         self._check(_lib.siso_kv_tree(self._h, batch._ref, parent.data_ptr(), mask.data_ptr(), depth.data_ptr()))
@@ -720,7 +720,8 @@ class PagedKV:
                 target.stride(1) != 1:
             raise ValueError(f"target: expected a [{rows}, vocab] float32 or bfloat16 tensor on {self.device}, entries of a row side by side")
         out_accepted = self._out(out_accepted, (batch.n,), torch.int32, "out_accepted")
-        out_rows, out_tokens = (self._out(t, (rows,), torch.int32, what) for t, what in ((out_rows, "out_rows"), (out_tokens, "out_tokens")))
+        out_rows = torch.empty_like(tokens) if out_rows is None else self._out(out_rows, (rows,), torch.int32, "out_rows")  # (a microsecond less than by shape)
+        out_tokens = torch.empty_like(tokens) if out_tokens is None else self._out(out_tokens, (rows,), torch.int32, "out_tokens")
         if self._elsewhere():
             self._used(tree.parent, tokens, target, u, out_accepted, out_rows, out_tokens, *batch.tensors)
         self._check(_lib.siso_kv_verify_tree(self._h, batch._ref, tree.parent.data_ptr(), tokens.data_ptr(), target.shape[1],
