@@ -197,3 +197,30 @@ def test_keys_that_are_infinite_where_they_weigh_nothing(siso, rows, apart):  # 
     s.kv.weigh(s.batch, wide[:, :, :64], lse, s.weights, fresh=ints([0]))
     mass = s.weights.mass.cpu()[0, s.pages.cpu()[0, 0].long(), 0]
     assert mass[10] == 0 and (mass[:10] > 0).all()
+
+
+def test_thousands_of_sequences(siso):  # noqa: F811
+    """More sequences than a workgroup plans for at a time: trees, their paths, weights and eviction."""
+    print("case: thousands of sequences", flush=True)
+    rng = random.Random(8)
+    n = 1500
+    new = [rng.randrange(0, 4) for _ in range(n)]
+    length = [m + rng.randrange(0, 20) for m in new]
+    s = Trees(siso, "bf16", 8, 1, 16, new, length, seed=17)
+    s.write()
+    q = s.queries(2)
+    s.check_tree(q, label="thousands")
+    first, tokens = s.batch.first.tolist(), [rng.randrange(5) for _ in range(sum(new))]
+    target = torch.rand(sum(new), 5, generator=torch.Generator().manual_seed(5))
+    for u in (None, torch.rand(sum(new), generator=torch.Generator().manual_seed(6))):
+        accepted, path, out = (x.tolist() for x in s.kv.verify_tree(s.batch, s.tree, ints(tokens), target.to(DEV), None if u is None else u.to(DEV)))
+        for b in range(n):
+            r = slice(first[b], first[b + 1])
+            assert (accepted[b], path[r], out[r]) == oracle.verify(s.parents[b], tokens[r], target[r].double().numpy(), None if u is None else u[r].numpy())
+    w = Weighed(siso, "bf16", 8, 1, 16, new, length, seed=17)
+    w.write()
+    w.start()
+    lse = w.lse_of(q)
+    w.kv.weigh(w.batch, q.to(DEV), lse, w.weights)
+    w.check_weigh(q, lse, label="thousands")
+    Full(siso, "fp8", 8, 1, 16, length, seed=18).check(9, 3, 1, label="thousands")
