@@ -824,7 +824,7 @@ __device__ __forceinline__ bool kv_chunk_tile(const KvAttend &a, const KvPieces 
 
 // Trees of up to 64 sequences: every workgroup knows all lengths, and cuts the tiles so that all pieces together are as many as run at once, or twice as many,
 // and so on where there are more tiles than that: the smallest number of blocks with which they are no more.  (`tile_of`: number `index` counts tiles
-// and heads, not pieces.)  All tiles of a sequence go by its whole length.  False: there are not as many.
+// and heads, not pieces.)  All tiles of a sequence are cut as its whole length is.  False: there are not as many.
 // (24 trees of 35 to 64 rows, 4 heads for each of 8, behind 2,000 to 6,000 positions in 8 bits: 176 us, cut by the tiles that are likely 227.)
 template <int ROWS, int KEYS>
 __device__ __forceinline__ bool kv_tree_piece(const KvAttend &a, const KvPieces &p, long index, bool tile_of, KvTile &t, KvPiece &k) {
@@ -885,11 +885,12 @@ __device__ __forceinline__ bool kv_tree_piece(const KvAttend &a, const KvPieces 
     k.head = (int)(tile % (unsigned)heads);
     k.pieces = __builtin_amdgcn_readlane((int)pieces, at);
     k.from = __builtin_amdgcn_readlane(from, at);
-    k.blocks = __builtin_amdgcn_readlane((int)blocks, at);
     k.per = (int)per;
     k.part = (long)(unsigned)__builtin_amdgcn_readlane((int)before_parts, at) + tile;
     k.next_part = of_tiles;
     kv_tile<true>(a, (int)(tile / (unsigned)heads) * ROWS, ROWS, t);
+    // (a tile ends where its own rows do: of rows below position 0 there is no block, and no entry of the table.  Pieces behind that are empty.)
+    k.blocks = t.hi > k.from ? (t.hi - k.from + KEYS - 1) / KEYS : 0;
     return true;
 }
 // The piece of a workgroup of k_kv_attend_chunk, or the tile of one of k_kv_attend_join (`tile_of`).
