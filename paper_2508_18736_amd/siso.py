@@ -787,9 +787,10 @@ class PagedKV:
         self._whole(weights)
         if self._elsewhere():
             self._used(to, weights.mass, weights.born, *batch.tensors)
+        # (a tensor without elements has no address, and none means in place: any other will do, nothing is read there)
         self._check(_lib.siso_kv_evict(self._h, -1 if layer is None else self._layer(layer), batch._ref, keep, recent, early, weights.mass.data_ptr(),
-                                       None if weights.born is None else weights.born.data_ptr(), None if to is None else to.data_ptr(),
-                                       0 if to is None else to.shape[1]))
+                                       None if weights.born is None else weights.born.data_ptr(),
+                                       None if to is None else to.data_ptr() or batch.first.data_ptr(), 0 if to is None else to.shape[1]))
 
     def bad_pages(self) -> int:
         return self._check(_lib.siso_kv_bad_pages(self._h))
