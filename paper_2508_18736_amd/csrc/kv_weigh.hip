@@ -730,6 +730,7 @@ extern "C" int siso_kv_weigh(siso_kv *kv, int layer, const siso_kv_batch *batch,
     if (a.batch.n == 0 || a.batch.rows == 0) return SISO_OK;
     if (!q || !lse || !mass || ((uintptr_t)q & 1) || (((uintptr_t)lse | (uintptr_t)mass | (uintptr_t)born) & 3))
         return kv_fail(kv, SISO_EINVAL, "siso_kv_weigh: queries, lse and mass must be there, all aligned to their type");
+    if (a.batch.most == 0) return SISO_OK;  // (no position: launches without workgroups are errors)
     a.pool = kv_pool(kv, layer);
     a.q = (const bf16_t *)q;
     a.q_token = q_token;
