@@ -235,8 +235,9 @@ int siso_kv_keep(siso_kv *kv, int layer, const siso_kv_batch *batch, const int *
  *   decay:  0 to 1.  1: sums over all rows so far; 0: of this batch's rows alone, whatever mass held.
  *   mass:   device pointer, [layers][pages][kv_heads][page_tokens] floats: a position's is that of its slot.
  *   born:   the same of ints, or NULL.
- * A sequence without rows is left as it is, and so is all beyond its length.  No two sequences of a
- * batch may share a page.  Scores, within single precision's range as for siso_kv_attend, and sums are formed in single
+ * A sequence without rows is left as it is, and so is all beyond its length.  With a window and decay 1 pages whose positions
+ * are all ahead of `fresh` and of what its rows see are not met, as siso_kv_attend does not meet them: they may be given up.  No two sequences of a
+ * batch may share any other page.  Scores, within single precision's range as for siso_kv_attend, and sums are formed in single
  * precision, the sums in an order that does not depend on scheduling.  What a row does not see does not get anything of it: infinities and
  * NaN of a key or a row are found at the positions that the row sees.  Asynchronous.
  */

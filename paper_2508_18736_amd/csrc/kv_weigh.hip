@@ -20,6 +20,7 @@ struct KvWeigh {
     int heads, group;
     float scale;  // times log2(e): the weights are powers of two
     int window;
+    int ahead;  // what is ahead of it stays as it is, if it is not noted anew
     const float *lse;
     const int *fresh, *newest;
     float decay;
@@ -67,13 +68,20 @@ __device__ __forceinline__ bf16x8_t kv_codes_bf16(unsigned a, unsigned b) {  // 
 // ---------------------------------------------------------------------------- who does what
 // A lane's sequence, and how many units of work it has: of k_kv_weigh_few steps of positions, of k_kv_weigh_rows blocks of positions times stretches of
 // rows.  Lengths are known on the device only.
+// Positions ahead of `fresh` that no row sees keep their weight where it does not decay: they are not met (attention does not meet them either), their
+// pages may be given up, or be another sequence's by now.  The rest begins with the first block that has one of the others.
+__device__ __forceinline__ int kv_weigh_from(const KvWeigh &a, const KvSequence &s) {
+    if (!a.ahead) return 0;
+    const int seen = s.start - a.window + 1, fresh = a.fresh ? a.fresh[s.b] : s.start, from = fresh < seen ? fresh : seen;
+    return from > 0 ? from & ~(SISO_KV_BLOCK - 1) : 0;  // (below the length: the last row sees itself)
+}
 template <bool FEW>
 struct KvShare {
     using Count = typename std::conditional<FEW, unsigned, u64>::type;  // (of few rows there are at most 2^24 steps of a sequence, and 2^27 pieces of work)
-    int first, rows, length;
+    int first, rows, length, from;
     Count units;
     __device__ __forceinline__ void load(const KvWeigh &a, int b, int stretch) {
-        first = rows = length = 0;
+        first = rows = length = from = 0;
         units = 0;
         if (b >= a.batch.n) return;
         const KvSequence s = kv_sequence(a.batch, b);
@@ -81,8 +89,9 @@ struct KvShare {
         rows = s.rows;
         length = s.length;
         if (rows == 0 || length == 0 || (rows * a.group <= KV_WEIGH_FEW) != FEW) return;
-        if constexpr (FEW) units = ((unsigned)length + KV_STEP - 1) / KV_STEP;
-        else units = (u64)(((unsigned)length + a.block - 1) / (unsigned)a.block) * (((unsigned)(rows * a.group) + stretch - 1) / (unsigned)stretch);
+        from = kv_weigh_from(a, s);
+        if constexpr (FEW) units = ((unsigned)(length - from) + KV_STEP - 1) / KV_STEP;
+        else units = (u64)(((unsigned)(length - from) + a.block - 1) / (unsigned)a.block) * (((unsigned)(rows * a.group) + stretch - 1) / (unsigned)stretch);
     }
     // Pieces of work of the sequence, of all heads.
     __device__ __forceinline__ Count pieces(const KvWeigh &a, unsigned stretch) const {
@@ -159,6 +168,7 @@ __global__ __launch_bounds__(1024) void k_kv_weigh_plan(KvWeigh a) {
 struct KvWork {
     KvSequence s;
     int head;
+    int from;          // where the sequence's positions begin
     unsigned stretch;  // in steps of positions, or rows of work
     u64 in;            // which of the sequence's and head's
 };
@@ -200,6 +210,7 @@ __device__ __forceinline__ bool kv_weigh_find(const KvWeigh &a, u64 item, KvWork
     k.s.rows = __builtin_amdgcn_readlane(share.rows, at);
     k.s.length = __builtin_amdgcn_readlane(share.length, at);
     k.s.start = k.s.length - k.s.rows;
+    k.from = __builtin_amdgcn_readlane(share.from, at);
     const u64 before = (u64)(upto - mine);
     const u64 in = wanted - (((u64)(unsigned)__builtin_amdgcn_readlane((int)(before >> 32), at) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)before, at));
     k.in = kv_divide(in, (unsigned)a.pool.kv_heads);
@@ -305,9 +316,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 4 : 2) void k_kv_weigh_few(KvWeigh
     KvWork k;
     if (!kv_weigh_find<true>(a, (u64)a.item0 + blockIdx.x, k)) return;
     const int work = k.s.rows * a.group, tiles = (work + 31) >> 5;
-    const long begin = (long)k.in * k.stretch * KV_STEP;
+    const long begin = k.from + (long)k.in * k.stretch * KV_STEP;
     const int from = (int)begin, to = begin + (long)k.stretch * KV_STEP < k.s.length ? (int)(begin + (long)k.stretch * KV_STEP) : k.s.length;
-    // positions ahead of every row's window are not read
+    // positions ahead of every row's window (that decay, or are noted anew) have no products
     const long seen_from = a.window > 0 ? (long)k.s.start - a.window + 1 : 0;
     int at = from + 32 * w;
     auto pages_of = [&](int p, int (&page)[2]) {
@@ -448,7 +459,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_weigh_rows(KvWeigh a) {
         if (!kv_weigh_find<false>(a, item, k)) return;
         const unsigned stretches = ((unsigned)(k.s.rows * a.group) + k.stretch - 1) / k.stretch;
         const unsigned block = (unsigned)kv_divide(k.in, stretches), piece = (unsigned)(k.in - (u64)block * stretches);
-        const int p0 = (int)(block * BLOCK), at = p0 + 32 * SUBS * w;  // the block's positions, this wave's
+        const int p0 = k.from + (int)(block * BLOCK), at = p0 + 32 * SUBS * w;  // the block's positions, this wave's
         bf16x8_t kx[SUBS][NS];
         float scale[SUBS], sum[SUBS] = {};
 #pragma unroll
@@ -741,6 +752,7 @@ extern "C" int siso_kv_weigh(siso_kv *kv, int layer, const siso_kv_batch *batch,
     a.group = heads / kv->kv_heads;
     a.scale = copysignf(fminf(fmaxf(fabsf(scale) * 1.44269504089f, 1.17549435e-38f), 3.40282347e38f), scale);  // (as siso_kv_attend takes it)
     a.window = window < a.batch.most ? window : 0;
+    a.ahead = a.window > 0 && decay == 1.f;
     a.lse = lse;
     a.fresh = fresh;
     a.newest = newest;
