@@ -91,6 +91,10 @@ __global__ __launch_bounds__(NT) void k_kv_choose(KvEvict a, int room) {
     unsigned *const ages = numbers + 4 * quads;  // (if there is room)
     for (int i = t; i < TURNS * KV_DIGIT; i += NT) counts[0][i] = 0;
     auto largest = [](int x, int y) __attribute__((always_inline)) { return x > y ? x : y; };
+    // (a page that is none is counted at its first four positions, where they are first asked for: what is never kept of it nothing else meets)
+    auto met = [&](int q, unsigned at) __attribute__((always_inline)) {
+        if (at == KV_NOWHERE && u.head == 0 && (4 * q & ((1 << a.pool.shift) - 1)) == 0) atomicAdd(a.pool.bad, 1ull);
+    };
     // Four positions' places and what is there, AHEAD times; f(quad, place, weights, ages).
     constexpr int AHEAD = 4;
     auto each = [&](bool weights, bool times, auto f) __attribute__((always_inline)) {
@@ -109,7 +113,10 @@ __global__ __launch_bounds__(NT) void k_kv_choose(KvEvict a, int room) {
             }
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
-                if (q0 + k * NT < quads) f(q0 + k * NT, at[k], weight[k], when[k]);
+                if (q0 + k * NT < quads) {
+                    met(q0 + k * NT, at[k]);
+                    f(q0 + k * NT, at[k], weight[k], when[k]);
+                }
         }
     };
     int newest = length - 1;
@@ -193,6 +200,7 @@ __global__ __launch_bounds__(NT) void k_kv_choose(KvEvict a, int room) {
 #pragma unroll 1
             for (int q = t; q < quads; q += NT) {
                 const u32x4_t x = four(q);
+                if (!HERE && turn == 0 && !born && x[0] == 0) met(q, KV_NOWHERE);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (turn == 0 || ((x[j] ^ bar) >> (shift + bits)) == 0) atomicAdd(&counts[turn][(x[j] >> shift) & ((1u << bits) - 1)], 1u);
