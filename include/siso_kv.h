@@ -58,8 +58,8 @@ typedef struct siso_kv siso_kv; /* opaque; owns the pages on the device */
  *   pages:  device pointer, [n][width] page numbers (NULL length and pages: siso_kv_verify);
  *           width * page_tokens is at most 2^31 - 2^25 (SISO_EINVAL otherwise).
  *   max_new, max_length: no sequence has more new tokens / more tokens (0: not known; rows
- *           and width * page_tokens are taken).  They size launches: a sequence of more rows
- *           than max_new may be left out, max_length only weighs on speed.
+ *           and width * page_tokens are taken).  They size launches: where a sequence has more rows
+ *           than max_new, sequences of the batch may be left out; max_length only weighs on speed.
  * The arrays are read when the work runs.  What does not keep to these ranges is never
  * read or written at: lengths are taken as the closest allowed one, positions below 0 are
  * no positions (nothing is written; a query there sees nothing), and a page number that
@@ -206,7 +206,7 @@ int siso_kv_attend_tree(siso_kv *kv, int layer, const siso_kv_batch *batch, cons
  *   out_rows:     device pointer, [rows] ints: per sequence the rows of the walk, 0 first, then -1.
  *   out_tokens:   device pointer, [rows] ints: per sequence the tokens that stand, the token that follows, then -1.
  * With that, and siso_kv_keep, the sequence stands at length[b] - m + 1 + out_accepted[b] tokens.
- * Only rows that the walk comes to are read.  Sums are formed in double precision.  Asynchronous.
+ * Rows that the walk does not come to do not count, though they may be read.  Sums are formed in double precision.  Asynchronous.
  */
 int siso_kv_verify_tree(siso_kv *kv, const siso_kv_batch *batch, const int *parent, const int *tokens, int vocab, int type,
                         const void *target, long target_stride, const float *u, int *out_accepted, int *out_rows, int *out_tokens);
